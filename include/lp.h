@@ -53,7 +53,8 @@ extern "C" {
 #define LP_ERR_UNSUPPORTED (-3) /* head_dim not in {64, 128}, sizes past 32-bit addressing    */
 #define LP_ERR_HIP (-4)         /* a HIP call failed; see lp_last_hip_error()                 */
 #define LP_ERR_NOMEM (-5)       /* host allocation failed                                     */
-#define LP_ERR_LIMIT (-6)       /* beyond the fixed scratch of a non-allocating entry point   */
+#define LP_ERR_LIMIT (-6)       /* beyond the fixed scratch of a non-allocating entry point,   */
+                                /* more than LP_MAX_REQUESTS requests                          */
 
 #define LP_MAX_PARTS 64
 
@@ -290,6 +291,73 @@ int lp_linear(const void *x, const void *w, const float *bias, void *y, int64_t 
  */
 int lp_qk_norm_rope(void *x, const float *gain, float eps, const lp_rope *rope, int64_t n_tokens, int32_t heads,
                     int32_t head_dim, int64_t stride_tok, int64_t stride_head, void *stream);
+
+/*
+ * ---- Blocks over the tokens of several requests at once --------------------------------------
+ * A server packs the rows (tokens) of several requests one after the other and runs a block over
+ * all of them; a guided pair is two requests.  What differs between them -- the scale, shift and
+ * gate that a request's timestep gives, its adapter, its patch grid -- is looked up by the row's
+ * request.  None of this is the paper's: it is the common form of an adaptive-norm DiT block and of
+ * low-rank adapters, stated here.
+ */
+#define LP_MAX_REQUESTS 64
+
+/* Request r owns rows start[r] .. start[r + 1] - 1 of every packed buffer.  start: host, count + 1
+ * values, start[0] = 0, not decreasing (equal: a request without rows), the last below 2^31 - 1 (else
+ * LP_ERR_UNSUPPORTED); count 0 .. LP_MAX_REQUESTS (else LP_ERR_LIMIT).  Rows from start[count] on are
+ * neither read nor written.  Read during the call only, like every other host argument here; a call captured into
+ * a graph keeps the layout it was captured with. */
+typedef struct lp_requests {
+    int32_t count;
+    const int64_t *start;
+} lp_requests;
+
+#define LP_BF16 0 /* element types of the residual stream */
+#define LP_F32 1
+
+#define LP_NORM_LAYER 0 /* (x - mean) / sqrt(mean (x - mean)^2 + eps), over a row's d elements */
+#define LP_NORM_RMS 1   /* x / sqrt(mean x^2 + eps)                                            */
+
+/* One normalisation: norm(x) * weight + bias.  weight, bias: device, binary32 [d], or NULL (1, 0). */
+typedef struct lp_norm {
+    int32_t kind;
+    float eps; /* >= 0 */
+    const float *weight, *bias;
+} lp_norm;
+
+/* The vectors that a request's conditioning gives, device, binary32: element e of request r at r * stride + e.
+ * NULL: gate 1, scale 0, shift 0.  stride >= d, or 0: one vector for all requests. */
+typedef struct lp_modulation {
+    const float *gate, *scale, *shift;
+    int64_t stride;
+} lp_modulation;
+
+/*
+ * y[i] = norm(x[i]) * (1 + scale[r]) + shift[r] with norm's own weight and bias inside, r the request of row i.
+ * x: device, x_type, row i at i * stride_x; y: device, bf16, row i at i * stride_y (strides in
+ * elements, >= d).  norm: host.  modulation: host, or NULL; its gate is not used.  d 1 .. 16384 (else
+ * LP_ERR_UNSUPPORTED).  y may be x (x_type LP_BF16, equal strides).  Any address that is aligned to its
+ * element type is taken; with d and all strides multiples of 8 and 16-byte aligned addresses
+ * (modulation included, its stride a multiple of 4) rows move in 16-byte pieces.
+ * Mean and variance are binary32 sums over the row held in registers, the variance about the mean; one rounding, on
+ * store.  A row that holds an infinity or a NaN comes out unspecified, other rows are not affected.
+ */
+int lp_norm_modulate(const void *x, int32_t x_type, void *y, const lp_requests *requests, int32_t d, int64_t stride_x,
+                     int64_t stride_y, const lp_norm *norm, const lp_modulation *modulation, void *stream);
+
+/*
+ * The end of one half of a block and the start of the next, in one pass over the rows:
+ *   h_out[i] = h[i] + gate[r] * post(u[i])
+ *   y[i]     = norm(h_out[i]) * (1 + scale[r]) + shift[r]
+ * h, h_out: device, h_type, rows at i * stride_h and i * stride_h_out: the residual stream; h_out may be h (equal
+ * strides).  u: device, bf16, rows at i * stride_u: what the half computed.  y: device, bf16, rows at i * stride_y;
+ * NULL together with norm for the last residual, which nothing follows.  post: host, normalisation of u, or NULL for
+ * u itself.  y is formed from the binary32 sum, before it is rounded to h_type.  No other buffers may be the same.
+ * Everything else as lp_norm_modulate.
+ */
+int lp_gated_residual_norm(const void *h, int32_t h_type, const void *u, void *h_out, void *y, const lp_requests *requests,
+                           int32_t d, int64_t stride_h, int64_t stride_u, int64_t stride_h_out, int64_t stride_y,
+                           const lp_norm *post, const lp_norm *norm, const lp_modulation *modulation, void *stream);
 
 /*
  * lp_attention for callers that cannot allocate device memory or hand over a workspace

@@ -27,6 +27,9 @@ LP_ERR_HIP = -4
 LP_ERR_NOMEM = -5
 LP_ERR_LIMIT = -6
 LP_MAX_PARTS = 64
+LP_MAX_REQUESTS = 64
+LP_BF16, LP_F32 = 0, 1
+LP_NORM_LAYER, LP_NORM_RMS = 0, 1
 
 # every symbol include/lp.h declares
 EXPORTS = (
@@ -35,6 +38,7 @@ EXPORTS = (
     "lp_reconstruct_guided_step", "lp_reconstruct_guided_step_partition",
     "lp_attention", "lp_attention_batch", "lp_attention_workspace_size", "lp_attention_static",
     "lp_attention_static_scratch_bytes", "lp_qkv_projection", "lp_linear", "lp_qk_norm_rope",
+    "lp_norm_modulate", "lp_gated_residual_norm",
     "lp_strerror", "lp_last_hip_error", "lp_version",
 )
 
@@ -54,6 +58,18 @@ class lp_part_info(C.Structure):
 
 class lp_rope(C.Structure):
     _fields_ = [("grid", C.c_int32 * 3), ("offset", C.c_int32 * 3), ("split", C.c_int32 * 3), ("base", C.c_float)]
+
+
+class lp_requests(C.Structure):
+    _fields_ = [("count", C.c_int32), ("start", C.POINTER(C.c_int64))]
+
+
+class lp_norm(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("eps", C.c_float), ("weight", C.c_void_p), ("bias", C.c_void_p)]
+
+
+class lp_modulation(C.Structure):
+    _fields_ = [("gate", C.c_void_p), ("scale", C.c_void_p), ("shift", C.c_void_p), ("stride", C.c_int64)]
 
 
 class LPError(RuntimeError):
@@ -119,6 +135,11 @@ def _lib():
         lib.lp_linear.restype = C.c_int
         lib.lp_qk_norm_rope.argtypes = [vp, vp, C.c_float, C.POINTER(lp_rope), i64, i32, i32, i64, i64, vp]
         lib.lp_qk_norm_rope.restype = C.c_int
+        lib.lp_norm_modulate.argtypes = [vp, i32, vp, C.POINTER(lp_requests), i32, i64, i64, C.POINTER(lp_norm), C.POINTER(lp_modulation), vp]
+        lib.lp_norm_modulate.restype = C.c_int
+        lib.lp_gated_residual_norm.argtypes = [vp, i32, vp, vp, vp, C.POINTER(lp_requests), i32, i64, i64, i64, i64, C.POINTER(lp_norm),
+                                               C.POINTER(lp_norm), C.POINTER(lp_modulation), vp]
+        lib.lp_gated_residual_norm.restype = C.c_int
         lib.lp_attention_workspace_size.argtypes = [i32]
         lib.lp_attention_workspace_size.restype = i64
         lib.lp_strerror.argtypes = [C.c_int]
@@ -313,3 +334,50 @@ def lp_qk_norm_rope(x, gain, eps: float, rope: lp_rope, n_tokens: int, heads: in
                     stride_head: int, stream: Optional[int] = None) -> None:
     _check(_lib().lp_qk_norm_rope(_ptr(x), _ptr(gain), float(eps), C.byref(rope), int(n_tokens), int(heads), int(head_dim),
                                   int(stride_tok), int(stride_head), stream or None), "lp_qk_norm_rope")
+
+
+def make_requests(starts) -> lp_requests:
+    """Requests packed one after the other: request r owns rows starts[r] .. starts[r + 1] - 1."""
+    starts = [int(v) for v in starts]
+    r = lp_requests(max(len(starts) - 1, 0), (C.c_int64 * max(len(starts), 1))(*starts))
+    return r
+
+
+def make_norm(kind: int, eps: float, weight=None, bias=None) -> lp_norm:
+    """One normalisation; weight and bias are device vectors that the caller keeps."""
+    return lp_norm(int(kind), float(eps), _ptr(weight) or None, _ptr(bias) or None)
+
+
+def make_modulation(gate=None, scale=None, shift=None, stride: Optional[int] = None) -> lp_modulation:
+    """Vectors per request, device, binary32, which the caller keeps.  stride defaults to the row stride that the tensors
+    given have in common; a vector (one dimension) is that of every request."""
+    if stride is None:
+        strides = {int(t.stride(0)) if t.dim() > 1 else 0 for t in (gate, scale, shift) if t is not None}
+        if len(strides) > 1:
+            raise ValueError("gate, scale and shift need one row stride: %s" % sorted(strides))
+        stride = strides.pop() if strides else 0
+    return lp_modulation(_ptr(gate) or None, _ptr(scale) or None, _ptr(shift) or None, int(stride))
+
+
+def _ref(struct):
+    return None if struct is None else C.byref(struct)
+
+
+def lp_norm_modulate(x, x_type: int, y, requests: lp_requests, d: int, norm: lp_norm, modulation: Optional[lp_modulation] = None,
+                     stride_x: Optional[int] = None, stride_y: Optional[int] = None, stream: Optional[int] = None) -> None:
+    """Strides default to d."""
+    _check(_lib().lp_norm_modulate(_ptr(x) or None, int(x_type), _ptr(y) or None, _ref(requests), int(d), _or(stride_x, d), _or(stride_y, d),
+                                   _ref(norm), _ref(modulation), stream or None), "lp_norm_modulate")
+
+
+def lp_gated_residual_norm(h, h_type: int, u, h_out, y, requests: lp_requests, d: int, post: Optional[lp_norm], norm: Optional[lp_norm],
+                           modulation: Optional[lp_modulation] = None, stride_h: Optional[int] = None, stride_u: Optional[int] = None,
+                           stride_h_out: Optional[int] = None, stride_y: Optional[int] = None, stream: Optional[int] = None) -> None:
+    """Strides default to d."""
+    _check(_lib().lp_gated_residual_norm(_ptr(h) or None, int(h_type), _ptr(u) or None, _ptr(h_out) or None, _ptr(y) or None, _ref(requests),
+                                         int(d), _or(stride_h, d), _or(stride_u, d), _or(stride_h_out, d), _or(stride_y, d), _ref(post),
+                                         _ref(norm), _ref(modulation), stream or None), "lp_gated_residual_norm")
+
+
+def _or(stride, d: int) -> int:
+    return int(d) if stride is None else int(stride)
