@@ -7,6 +7,7 @@
 // the results, so that every element of x (h and u) is read once and every result written once.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "lp_device.h"
@@ -66,53 +67,52 @@ struct RowSum {
 };
 
 // A thread's elements: CH pieces of 8.  VEC 8: piece c is the 8 elements from 8 (c G + t) on, moved 16 bytes at a time; VEC 1: element j
-// of all of them is j G + t.  at(j) is the place of element j (of its piece's first, VEC 8).
+// of all of them is j G + t.  Rows are raw buffers of d elements: what lies past the end is read as 0 and not written, so that
+// no address is computed and no lane masked for an element, which in single elements took all registers there are (one
+// wavefront to a SIMD: 1111 x 1153 in 21.7 us).
+template <typename T>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t row_buffer(const T *row, int d) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(row), 0, d * int(sizeof(T)), 0x00020000);
+}
 template <int G, int CH, int VEC, typename T>
 struct Row {
     T v[8 * CH];
+    static constexpr int kPieces = 8 * sizeof(T) / 16, kPer = 16 / sizeof(T);
+    typedef __attribute__((ext_vector_type(kPer))) T Piece;
     __device__ __forceinline__ void load(const T *row, int t, int d) {
+        const __amdgpu_buffer_rsrc_t r = row_buffer(row, d);
+        if constexpr (VEC == 8) {
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            if constexpr (VEC == 8) {
-                const int e = 8 * (c * G + t);
-                constexpr int kPieces = 8 * sizeof(T) / 16, kPer = 16 / sizeof(T);
-                typedef __attribute__((ext_vector_type(kPer))) T Piece;
+            for (int c = 0; c < CH * kPieces; ++c) {
+                const int first = 8 * (c / kPieces) * G + (c % kPieces) * kPer;
+                const Piece p = __builtin_bit_cast(Piece, __builtin_amdgcn_raw_buffer_load_b128(r, t * 8 * sizeof(T), first * sizeof(T), 0));
 #pragma unroll
-                for (int p = 0; p < kPieces; ++p) {
-                    Piece piece{};
-                    if (e < d) piece = *reinterpret_cast<const Piece *>(row + e + p * kPer);
+                for (int i = 0; i < kPer; ++i) v[c * kPer + i] = p[i];
+            }
+        } else {
 #pragma unroll
-                    for (int i = 0; i < kPer; ++i) v[8 * c + p * kPer + i] = piece[i];
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int e = (8 * c + i) * G + t;
-                    v[8 * c + i] = e < d ? row[e] : T(0.0f);
-                }
+            for (int j = 0; j < 8 * CH; ++j) {
+                if constexpr (sizeof(T) == 2) v[j] = __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b16(r, t * 2, j * G * 2, 0));
+                else v[j] = __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(r, t * 4, j * G * 4, 0));
             }
         }
     }
     __device__ __forceinline__ void store(T *row, int t, int d) const {
+        const __amdgpu_buffer_rsrc_t r = row_buffer(row, d);
+        if constexpr (VEC == 8) {
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            if constexpr (VEC == 8) {
-                const int e = 8 * (c * G + t);
-                constexpr int kPieces = 8 * sizeof(T) / 16, kPer = 16 / sizeof(T);
-                typedef __attribute__((ext_vector_type(kPer))) T Piece;
+            for (int c = 0; c < CH * kPieces; ++c) {
+                const int first = 8 * (c / kPieces) * G + (c % kPieces) * kPer;
+                Piece p;
 #pragma unroll
-                for (int p = 0; p < kPieces; ++p) {
-                    Piece piece;
+                for (int i = 0; i < kPer; ++i) p[i] = v[c * kPer + i];
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, p), r, t * 8 * sizeof(T), first * sizeof(T), 0);
+            }
+        } else {
 #pragma unroll
-                    for (int i = 0; i < kPer; ++i) piece[i] = v[8 * c + p * kPer + i];
-                    if (e < d) *reinterpret_cast<Piece *>(row + e + p * kPer) = piece;
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int e = (8 * c + i) * G + t;
-                    if (e < d) row[e] = v[8 * c + i];
-                }
+            for (int j = 0; j < 8 * CH; ++j) {
+                if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v[j]), r, t * 2, j * G * 2, 0);
+                else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v[j]), r, t * 4, j * G * 4, 0);
             }
         }
     }
@@ -138,6 +138,11 @@ __device__ __forceinline__ void normalise(float (&v)[N], int kind, float eps, fl
 }
 
 // G threads to a row, every group of them a contiguous stretch of rows.
+//
+// What bounds it: HBM.  13230 x 5120 in bf16 (271 MB) 53.6 us, 5.05 TB/s; the residual of 24570 x 5120 (1.01 GB) 179 us, 5.6 TB/s; 22380 x 1536 in
+// binary32 with norms on both sides (413 MB) 81 us, 5.1 TB/s, where a plain copy of 4 GiB reaches 4.7 TB/s.  The vectors of a
+// request, up to four times d in binary32, would be two to four times a row's own bytes from L2 for every row: a thread keeps its part of them in
+// registers, products of the weights and the modulation, and fetches them again when its stretch enters another request.
 template <int G, int CH, int VEC, typename X, bool RESIDUAL>
 __global__ __launch_bounds__(G > 256 ? G : 256) void norm_kernel(const NormArgs a) {
     constexpr int kThreads = G > 256 ? G : 256, kGroups = kThreads / G, N = 8 * CH;
@@ -188,32 +193,43 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void norm_kernel(const NormArgs 
         }
     };
 
+    // The next row is sent for before this one's sums, whose exchanges it then arrives under; not with 1024 threads to a row, which
+    // have 128 registers each.
+    constexpr bool kAhead = G < 1024;
+    const X *xs = static_cast<const X *>(a.x);
+    Row<G, CH, VEC, X> x;
+    Row<G, CH, VEC, __bf16> u;
+    auto send = [&](int r) {
+        x.load(xs + int64_t(r) * a.stride_x, t, a.d);
+        if constexpr (RESIDUAL) u.load(a.u + int64_t(r) * a.stride_u, t, a.d);
+    };
+    if (kAhead && row < last) send(row);
     for (; row < last; ++row) {
+        if (!kAhead) send(row);
         if (row >= request_end) {
             const int request = request_of(ends, row);
             request_end = __builtin_amdgcn_readlane(ends, request);
             vectors(request);
         }
-        Row<G, CH, VEC, X> x;
-        x.load(static_cast<const X *>(a.x) + int64_t(row) * a.stride_x, t, a.d);
         float v[N];
         if constexpr (RESIDUAL) {
-            Row<G, CH, VEC, __bf16> u;
-            u.load(a.u + int64_t(row) * a.stride_u, t, a.d);
 #pragma unroll
             for (int j = 0; j < N; ++j) v[j] = float(u.v[j]);
+            Row<G, CH, VEC, X> h = x;
+            if (kAhead && row + 1 < last) send(row + 1);
             if (a.post != kNone) normalise(v, a.post, a.post_eps, a.inv_d, sum, live);
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                v[j] = float(x.v[j]) + (gate[j] * v[j] + gate_bias[j]);
-                x.v[j] = X(v[j]);
+                v[j] = float(h.v[j]) + (gate[j] * v[j] + gate_bias[j]);
+                h.v[j] = X(v[j]);
             }
-            x.store(static_cast<X *>(a.h_out) + int64_t(row) * a.stride_h_out, t, a.d);
+            h.store(static_cast<X *>(a.h_out) + int64_t(row) * a.stride_h_out, t, a.d);
 #pragma unroll
             for (int j = 0; j < N; ++j) v[j] = live(j) ? v[j] : 0.0f;
         } else {
 #pragma unroll
             for (int j = 0; j < N; ++j) v[j] = float(x.v[j]);
+            if (kAhead && row + 1 < last) send(row + 1);
         }
         if (a.norm == kNone) continue;
         normalise(v, a.norm, a.eps, a.inv_d, sum, live);
@@ -222,6 +238,19 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void norm_kernel(const NormArgs 
         for (int j = 0; j < N; ++j) y.v[j] = __bf16(v[j] * mul[j] + add[j]);
         y.store(a.y + int64_t(row) * a.stride_y, t, a.d);
     }
+}
+
+// Workgroups of `groups` rows at a time.  Few rows: one each.  Beyond two workgroups to a compute unit every group takes two rows at least
+// and fetches its request's vectors once for them, and all compute units have as many (1111 x 1153 with norms on both sides 8.2 us, 10.5 with a row each; 4000 x 1536
+// 6.4 and 6.7).  At most 4096 threads to a compute unit, twice what can run at a time, which evens out their ends: 13230 x 5120 53.6 us,
+// 57.0 with 2048, 59.4 with 1024.  8192 for the residual in whole pieces, whose rows are four streams instead of two: 24570 x 5120 179.4
+// us, 190.5 with 4096, 199 with 2048 (20000 x 3584 158 and 165; 13230 x 5120 without the residual 54.0 and 53.6; 12000 x 1153 in single elements
+// 46 and 43; 9000 x 16384, 1024 threads to a row, 366 and 358).
+uint32_t workgroups(int64_t n, int groups, int threads, int most_threads, int cus) {
+    const int64_t one_each = (n + groups - 1) / groups, few = 2 * int64_t(cus), most = int64_t(cus) * (most_threads / threads);
+    if (one_each <= few) return uint32_t(one_each);
+    const int64_t two_each = n / (2 * groups) / cus * cus;
+    return uint32_t(std::min(most, std::max(few, two_each)));
 }
 
 template <int G, int CH, int VEC>
@@ -233,8 +262,8 @@ int launch(const NormArgs &a, bool f32, bool residual, hipStream_t stream) {
                                      : reinterpret_cast<const void *>(&norm_kernel<G, CH, VEC, __bf16, true>))
                               : (f32 ? reinterpret_cast<const void *>(&norm_kernel<G, CH, VEC, float, false>)
                                      : reinterpret_cast<const void *>(&norm_kernel<G, CH, VEC, __bf16, false>));
-    const int64_t most = int64_t(cus) * (2048 / kThreads), wanted = (int64_t(a.n) + kGroups - 1) / kGroups;
-    return lp::launch_kernel(fn, dim3(uint32_t(wanted < most ? wanted : most)), dim3(kThreads), 0, stream, a);
+    const int most_threads = residual && VEC == 8 && G < 1024 ? 8192 : 4096;
+    return lp::launch_kernel(fn, dim3(workgroups(a.n, kGroups, kThreads, most_threads, cus)), dim3(kThreads), 0, stream, a);
 }
 
 int run(const NormArgs &a, bool vec, bool f32, bool residual, hipStream_t stream) {
@@ -245,10 +274,16 @@ int run(const NormArgs &a, bool vec, bool f32, bool residual, hipStream_t stream
         if (a.d <= 2048) return launch<256, 1, 8>(a, f32, residual, stream);
         if (a.d <= 4096) return launch<256, 2, 8>(a, f32, residual, stream);
         if (a.d <= 6144) return launch<256, 3, 8>(a, f32, residual, stream);
+        if (a.d <= 8192) return launch<512, 2, 8>(a, f32, residual, stream);
         return launch<1024, 2, 8>(a, f32, residual, stream);
     }
+    // single elements: what lies past the row's end costs an instruction each, so that the steps are finer (12000 x 1153 residual 43 us,
+    // 71 with 16 elements to a thread)
+    if (a.d <= 512) return launch<64, 1, 1>(a, f32, residual, stream);
     if (a.d <= 1024) return launch<64, 2, 1>(a, f32, residual, stream);
+    if (a.d <= 2048) return launch<256, 1, 1>(a, f32, residual, stream);
     if (a.d <= 4096) return launch<256, 2, 1>(a, f32, residual, stream);
+    if (a.d <= 8192) return launch<512, 2, 1>(a, f32, residual, stream);
     return launch<1024, 2, 1>(a, f32, residual, stream);
 }
 
