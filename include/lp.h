@@ -312,6 +312,55 @@ typedef struct lp_requests {
     const int64_t *start;
 } lp_requests;
 
+/*
+ * A low-rank adapter of a projection with weights W [d_out, d_in]: the projection of a row x becomes
+ *   W x + scale * up (down x).
+ * down: device, bf16 [rank, d_in]; up: device, bf16 [d_out, rank], both 16-byte aligned.  rank 0: none (the
+ * addresses are not looked at); otherwise a multiple of 8 up to LP_MAX_ADAPTER_RANK (else LP_ERR_UNSUPPORTED: an adapter of
+ * another rank is passed with zeros up to the next multiple).  scale finite.
+ */
+#define LP_MAX_ADAPTER_RANK 256
+typedef struct lp_adapter {
+    const void *down, *up;
+    int32_t rank;
+    float scale;
+} lp_adapter;
+
+/*
+ * lp_linear over the rows of several requests, each with its adapter beside the shared projection:
+ *   y[i] = w x[i] + bias + scale_r up_r (down_r x[i]),   r the request of row i.
+ * x, w, bias, y, d_in, d_out as lp_linear, x and y holding requests' rows.  adapters: host, one per request.
+ * Neighbouring requests with one and the same adapter cost no more than one of their common length.
+ * workspace: device scratch of at least lp_adapter_workspace_size(rows, the largest rank, 1) bytes,
+ * 16-byte aligned, contents irrelevant on entry and undefined on return (LP_ERR_INVALID_ARG if too small);
+ * not looked at when no request has an adapter.  Two calls that overlap in time must not share one; nor may the
+ * replays of two graphs that were captured with the same one.
+ * An infinity or a NaN in x, in down or in up makes rows of the requests that they belong to unspecified (typically NaN); rows
+ * of other requests are not affected.
+ * One small launch for the down products, whose results are kept as two bf16 each (2^-17 relative), then one for
+ * the rest: the adapters are further terms of w's sums, in binary32, with one rounding to bf16 on store.
+ */
+int lp_linear_adapters(const void *x, const void *w, const float *bias, void *y, const lp_requests *requests,
+                       int32_t d_in, int32_t d_out, const lp_adapter *adapters, void *workspace, int64_t workspace_bytes,
+                       void *stream);
+
+/*
+ * lp_qkv_projection over the rows of several requests, each with its patch grid and its adapter.
+ * An adapter of q | k | v: down bf16 [3 rank, d_model], whose thirds belong to q, k and v; up bf16
+ * [3 d_model, rank].  A part without adapter has zeros in up.  ropes: host, one per request: its grid (whose product is its number
+ * of rows; not looked at for a request without rows) and offset; split and base must be the same in all.
+ * workspace: lp_adapter_workspace_size(rows, the largest rank, 3) bytes.  Everything else as
+ * lp_qkv_projection and lp_linear_adapters.
+ */
+int lp_qkv_projection_adapters(const void *x, const void *w_qkv, const float *bias, const float *gain_q,
+                               const float *gain_k, float eps, const lp_rope *ropes, void *q, void *k, void *v,
+                               const lp_requests *requests, int32_t heads, int32_t head_dim, const lp_adapter *adapters,
+                               void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace for n_tokens rows and adapters of up to `rank`; sections: 1 (lp_linear_adapters) or 3
+ * (lp_qkv_projection_adapters).  128 bytes per row, section and 32 ranks, and 4224.  Negative LP_ERR_* on failure. */
+int64_t lp_adapter_workspace_size(int64_t n_tokens, int32_t rank, int32_t sections);
+
 #define LP_BF16 0 /* element types of the residual stream */
 #define LP_F32 1
 

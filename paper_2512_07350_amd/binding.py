@@ -28,6 +28,7 @@ LP_ERR_NOMEM = -5
 LP_ERR_LIMIT = -6
 LP_MAX_PARTS = 64
 LP_MAX_REQUESTS = 64
+LP_MAX_ADAPTER_RANK = 256
 LP_BF16, LP_F32 = 0, 1
 LP_NORM_LAYER, LP_NORM_RMS = 0, 1
 
@@ -38,7 +39,7 @@ EXPORTS = (
     "lp_reconstruct_guided_step", "lp_reconstruct_guided_step_partition",
     "lp_attention", "lp_attention_batch", "lp_attention_workspace_size", "lp_attention_static",
     "lp_attention_static_scratch_bytes", "lp_qkv_projection", "lp_linear", "lp_qk_norm_rope",
-    "lp_norm_modulate", "lp_gated_residual_norm",
+    "lp_norm_modulate", "lp_gated_residual_norm", "lp_linear_adapters", "lp_qkv_projection_adapters", "lp_adapter_workspace_size",
     "lp_strerror", "lp_last_hip_error", "lp_version",
 )
 
@@ -62,6 +63,10 @@ class lp_rope(C.Structure):
 
 class lp_requests(C.Structure):
     _fields_ = [("count", C.c_int32), ("start", C.POINTER(C.c_int64))]
+
+
+class lp_adapter(C.Structure):
+    _fields_ = [("down", C.c_void_p), ("up", C.c_void_p), ("rank", C.c_int32), ("scale", C.c_float)]
 
 
 class lp_norm(C.Structure):
@@ -135,6 +140,13 @@ def _lib():
         lib.lp_linear.restype = C.c_int
         lib.lp_qk_norm_rope.argtypes = [vp, vp, C.c_float, C.POINTER(lp_rope), i64, i32, i32, i64, i64, vp]
         lib.lp_qk_norm_rope.restype = C.c_int
+        lib.lp_linear_adapters.argtypes = [vp, vp, vp, vp, C.POINTER(lp_requests), i32, i32, C.POINTER(lp_adapter), vp, i64, vp]
+        lib.lp_linear_adapters.restype = C.c_int
+        lib.lp_qkv_projection_adapters.argtypes = [vp, vp, vp, vp, vp, C.c_float, C.POINTER(lp_rope), vp, vp, vp, C.POINTER(lp_requests), i32,
+                                                   i32, C.POINTER(lp_adapter), vp, i64, vp]
+        lib.lp_qkv_projection_adapters.restype = C.c_int
+        lib.lp_adapter_workspace_size.argtypes = [i64, i32, i32]
+        lib.lp_adapter_workspace_size.restype = i64
         lib.lp_norm_modulate.argtypes = [vp, i32, vp, C.POINTER(lp_requests), i32, i64, i64, C.POINTER(lp_norm), C.POINTER(lp_modulation), vp]
         lib.lp_norm_modulate.restype = C.c_int
         lib.lp_gated_residual_norm.argtypes = [vp, i32, vp, vp, vp, C.POINTER(lp_requests), i32, i64, i64, i64, i64, C.POINTER(lp_norm),
@@ -341,6 +353,51 @@ def make_requests(starts) -> lp_requests:
     starts = [int(v) for v in starts]
     r = lp_requests(max(len(starts) - 1, 0), (C.c_int64 * max(len(starts), 1))(*starts))
     return r
+
+
+def make_adapters(adapters):
+    """The adapters of the requests in order: (down, up, scale) with device tensors (the rank is up's second dimension) that the
+    caller keeps, or None."""
+    out = (lp_adapter * max(len(adapters), 1))()
+    for i, ad in enumerate(adapters):
+        if ad is not None:
+            down, up, scale = ad
+            if down.dim() != 2 or up.dim() != 2 or down.shape[0] % up.shape[1] or not (down.is_contiguous() and up.is_contiguous()):
+                raise ValueError("adapter %d: down [sections * rank, d_in] and up [d_out, rank], contiguous" % i)
+            out[i] = lp_adapter(_ptr(down), _ptr(up), int(up.shape[1]), float(scale))
+    return out
+
+
+def lp_adapter_workspace_size(n_tokens: int, rank: int, sections: int = 1) -> int:
+    n = int(_lib().lp_adapter_workspace_size(int(n_tokens), int(rank), int(sections)))
+    if n < 0:
+        raise LPError(n, "lp_adapter_workspace_size")
+    return n
+
+
+def _per_request(table, requests: lp_requests, what: str):
+    """A host table of structures, one for each request: the library reads as many as there are requests."""
+    if table is not None and requests is not None and len(table) < requests.count:
+        raise ValueError("%d %s for %d requests" % (len(table), what, requests.count))
+    return table
+
+
+def lp_linear_adapters(x, w, bias, y, requests: lp_requests, d_in: int, d_out: int, adapters, workspace=None, workspace_bytes: int = 0,
+                       stream: Optional[int] = None) -> None:
+    """adapters: see make_adapters."""
+    _check(_lib().lp_linear_adapters(_ptr(x) or None, _ptr(w) or None, _ptr(bias) or None, _ptr(y) or None, _ref(requests), int(d_in), int(d_out),
+                                     _per_request(adapters, requests, "adapters"), _ptr(workspace) or None, int(workspace_bytes), stream or None),
+           "lp_linear_adapters")
+
+
+def lp_qkv_projection_adapters(x, w_qkv, bias, gain_q, gain_k, eps: float, ropes, q, k, v, requests: lp_requests, heads: int, head_dim: int,
+                               adapters, workspace=None, workspace_bytes: int = 0, stream: Optional[int] = None) -> None:
+    """ropes: one lp_rope (make_rope) for each request; adapters: see make_adapters."""
+    ropes = _per_request((lp_rope * max(len(ropes), 1))(*ropes), requests, "ropes")
+    _check(_lib().lp_qkv_projection_adapters(_ptr(x) or None, _ptr(w_qkv) or None, _ptr(bias) or None, _ptr(gain_q) or None, _ptr(gain_k) or None,
+                                             float(eps), ropes, _ptr(q) or None, _ptr(k) or None, _ptr(v) or None, _ref(requests), int(heads),
+                                             int(head_dim), _per_request(adapters, requests, "adapters"), _ptr(workspace) or None,
+                                             int(workspace_bytes), stream or None), "lp_qkv_projection_adapters")
 
 
 def make_norm(kind: int, eps: float, weight=None, bias=None) -> lp_norm:

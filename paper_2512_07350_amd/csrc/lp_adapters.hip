@@ -1,0 +1,315 @@
+// Projections of several requests' tokens with a low-rank adapter of each beside the shared weights, for gfx950:
+//
+//   lp_linear_adapters           y = x W^T + b + s_r (x D_r^T) U_r^T
+//   lp_qkv_projection_adapters   the same in the sections q | k | v, q and k normalised and rotated
+//
+// with r the request that a row belongs to.  Two launches: adapter_down_kernel forms t = s_r x D_r^T of the rows that have an
+// adapter (and looks over every U_r), and the product of lp_gemm.h takes t and U_r as further k-tiles.  The second thus costs a k-tile of 64 for every
+// 32 ranks beside d_in / 64 of them, and no pass over y.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "lp_gemm.h"
+
+namespace {
+
+// ---- the down products
+
+struct DownRun {
+    int32_t start, rank;                 // as AdapterRun
+    int32_t first, first_look;           // the run's first workgroup, that of those that look over U
+    float scale;
+    const __bf16 *down, *up;             // D [sections * rank, d_in], U [d_out, rank]
+};
+struct DownArgs {
+    const __bf16 *x;
+    __bf16 *t;                           // see AdaptedArgs
+    uint32_t *control;
+    int32_t t_row, t_blocks, d_in, d_out, sections, looks;
+    DownRun run[LP_MAX_REQUESTS + 1];
+};
+
+// 16 bytes of U to a workgroup's look, in pieces of which a run has at most kLooks.
+__host__ __device__ int32_t look_pieces(int64_t pieces) {
+    const int64_t by_size = (pieces + 4095) / 4096;
+    return int32_t(by_size < kLooks ? by_size : kLooks);
+}
+
+using DownTile = Tiling<2, 2, 2, 1, 8, kSplitK>;         // 64 rows of D x 32 tokens, four wavefronts sharing k
+
+// Whether part of a run's U holds an infinity or a NaN, to its word of the control block; 64 KB to a workgroup up to 1 MB.
+__device__ void look_over(const DownArgs &a, int wg) {
+    const int r = __builtin_amdgcn_readfirstlane(__popcll(__ballot(a.run[threadIdx.x % 64].first_look <= wg))) - 1;
+    const int part = wg - a.run[r].first_look;
+    const int64_t pieces = int64_t(a.d_out) * a.run[r].rank / 8;
+    const int parts = look_pieces(pieces);
+    const uint4 *u = reinterpret_cast<const uint4 *>(a.run[r].up);
+    const int64_t last = pieces * (part + 1) / parts;
+    uint32_t bad = 0;
+    auto look = [&](uint32_t two) { bad |= uint32_t((two & 0x7f80u) == 0x7f80u) | uint32_t((two & 0x7f800000u) == 0x7f800000u); };
+#pragma unroll 8
+    for (int64_t i = pieces * part / parts + threadIdx.x; i < last; i += DownTile::kThreads) {
+        const uint4 p = u[i];
+        look(p.x);
+        look(p.y);
+        look(p.z);
+        look(p.w);
+    }
+    const int any = __syncthreads_or(int(bad));
+    uint32_t *words = a.control + kControlNan + r * kLooks;
+    if (threadIdx.x == 0) words[part] = uint32_t(any);
+    if (part == 0 && int(threadIdx.x) >= parts && threadIdx.x < kLooks) words[threadIdx.x] = 0;
+    if (wg == 0 && threadIdx.x < kControlNan) a.control[threadIdx.x] = 0x7fc07fc0u;
+}
+
+__global__ __launch_bounds__(DownTile::kThreads, 1) void adapter_down_kernel(const DownArgs a) {
+    using C = DownTile;
+    if (int(blockIdx.x) < a.looks) return look_over(a, int(blockIdx.x));
+    const int wg = int(blockIdx.x) - a.looks;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    const uint32_t lds0 = uint32_t(uintptr_t(LP_LDS_PTR(unsigned char, smem)));
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, col = lane % 16, quad = lane / 16;
+    // the run of this workgroup: the last one that starts with it or before
+    const int r = __builtin_amdgcn_readfirstlane(__popcll(__ballot(a.run[lane].first <= wg))) - 1;
+    const int rank = a.run[r].rank, rows = a.sections * rank, f_tiles = (rows + C::kF - 1) / C::kF, j = wg - a.run[r].first;
+    const int f0 = j % f_tiles * C::kF, t0 = a.run[r].start + j / f_tiles * C::kT;
+    GemmArgs g{};
+    g.x = a.x;
+    g.w = a.run[r].down;
+    g.n = a.run[r + 1].start;
+    g.d_in = a.d_in;
+    g.d_out = rows;
+    f32x4 acc[C::FB][C::TB];
+    product_split_k<C>(lds0, g, f0, t0, wave, lane, acc);
+    const float scale = a.run[r].scale;
+    const int tok = t0 + wave % C::WT * 16 + col;
+#pragma unroll
+    for (int f = 0; f < C::FB; ++f) {
+        const int row = f0 + (wave / C::WT * C::FB + f) * 16 + 4 * quad;   // of D; four of them, of one section
+        if (row >= rows || tok >= g.n) continue;
+        const int section = row / rank, at = row - section * rank;
+        const f32x4 v = acc[f][0] * scale;
+        const bf16x4 hi = __builtin_convertvector(v, bf16x4), lo = __builtin_convertvector(v - __builtin_convertvector(hi, f32x4), bf16x4);
+        __bf16 *to = a.t + int64_t(tok) * (a.t_row / 2) + (section * a.t_blocks + at / kRanks) * (2 * kRanks) + at % kRanks;
+        *reinterpret_cast<bf16x4 *>(to) = hi;
+        *reinterpret_cast<bf16x4 *>(to + kRanks) = lo;
+    }
+}
+
+// ---- the requests' adapters
+
+int64_t t_row_bytes(int32_t rank, int32_t sections) { return int64_t(sections) * ((rank + kRanks - 1) / kRanks) * (4 * kRanks); }
+
+// Neighbouring requests with one adapter as runs, with the down products' launch.
+struct Runs {
+    RequestTable requests;
+    int32_t runs = 0, largest = 0;       // runs; the largest rank
+    int64_t workgroups = 0;              // of the down products
+    DownArgs down{};
+    AdapterRun run[LP_MAX_REQUESTS + 1];
+};
+
+int make_runs(const lp_requests *requests, const lp_adapter *adapters, int32_t d_in, int32_t d_out, int32_t sections, Runs *out) {
+    const int rc = make_request_table(requests, &out->requests);
+    if (rc != LP_OK) return rc;
+    const RequestTable &q = out->requests;
+    if (q.count > 0 && adapters == nullptr) return LP_ERR_INVALID_ARG;
+    for (int r = 0; r < q.count; ++r) {
+        const lp_adapter &ad = adapters[r];
+        if (ad.rank < 0) return LP_ERR_INVALID_ARG;
+        if (ad.rank > LP_MAX_ADAPTER_RANK || ad.rank % 8 != 0) return LP_ERR_UNSUPPORTED;
+        if (ad.rank > 0 && (ad.down == nullptr || ad.up == nullptr || !aligned16(ad.down) || !aligned16(ad.up) || !std::isfinite(ad.scale)))
+            return LP_ERR_INVALID_ARG;
+    }
+    const lp_adapter *last = nullptr;
+    for (int r = 0; r < q.count; ++r) {
+        const lp_adapter &ad = adapters[r];
+        if (q.start[r + 1] == q.start[r]) continue;
+        const bool same = last != nullptr && last->rank == ad.rank &&
+                          (ad.rank == 0 || (last->down == ad.down && last->up == ad.up && last->scale == ad.scale));
+        last = &ad;
+        if (same) continue;
+        const int i = out->runs++;
+        out->run[i] = AdapterRun{q.start[r], ad.rank, static_cast<const __bf16 *>(ad.up)};
+        out->down.run[i] = DownRun{q.start[r], ad.rank, 0, 0, ad.scale, static_cast<const __bf16 *>(ad.down), static_cast<const __bf16 *>(ad.up)};
+        if (ad.rank > out->largest) out->largest = ad.rank;
+    }
+    const int32_t n = int32_t(q.rows());
+    for (int i = out->runs; i <= LP_MAX_REQUESTS; ++i) {
+        out->run[i] = AdapterRun{i == out->runs ? n : INT32_MAX, 0, nullptr};
+        out->down.run[i] = DownRun{i == out->runs ? n : INT32_MAX, 0, INT32_MAX, INT32_MAX, 0.0f, nullptr, nullptr};
+    }
+    for (int i = 0; i < out->runs; ++i) {
+        const int64_t tokens = (int64_t(out->run[i + 1].start) - out->run[i].start + DownTile::kT - 1) / DownTile::kT;
+        const int64_t rows = (int64_t(sections) * out->run[i].rank + DownTile::kF - 1) / DownTile::kF;
+        out->down.run[i].first = int32_t(out->workgroups);
+        out->workgroups += tokens * rows;
+        out->down.run[i].first_look = out->down.looks;
+        out->down.looks += look_pieces(int64_t(d_out) * out->run[i].rank / 8);
+        if ((out->workgroups + out->down.looks) * DownTile::kThreads > lp::kMaxLaunchThreads) return LP_ERR_UNSUPPORTED;
+    }
+    out->down.d_in = d_in;
+    out->down.d_out = d_out;
+    out->down.sections = sections;
+    return LP_OK;
+}
+
+// The tiling of a call: pick_plan's, with the k-tiles of the adapters that a tile of t tokens takes on average.
+Plan pick_adapted(int32_t n, int32_t d_in, int32_t d_out, int32_t head_dim, int cus, int32_t runs, const AdapterRun *run) {
+    return pick_plan(n, d_out, false, cus, [&](int t) {
+        int64_t extra = 0;
+        for (int i = 0; i < runs; ++i) {
+            const int64_t first = run[i].start / t, last = (run[i + 1].start - 1) / t;
+            extra += (last - first + 1) * ((run[i].rank + kRanks - 1) / kRanks);
+        }
+        const int64_t tiles = (int64_t(n) + t - 1) / t;
+        return d_in / kBK + int((extra + tiles - 1) / tiles);
+    });
+}
+
+// What the calls share from here on: the workspace, the down products, the tilings.
+template <bool QKV, int HD>
+int project(AdaptedArgs<QKV> &a, Runs &runs, void *workspace, int64_t workspace_bytes, hipStream_t stream) {
+    const int64_t t_row = t_row_bytes(runs.largest, QKV ? 3 : 1);
+    if (runs.largest > 0 && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < kControlBytes + t_row * a.n)) return LP_ERR_INVALID_ARG;
+    int dev = 0;
+    const int cus = lp::device_compute_units(&dev);
+    if (cus <= 0) return LP_ERR_HIP;
+    if (runs.largest > 0) {
+        DownArgs &d = runs.down;
+        d.x = a.x;
+        d.control = static_cast<uint32_t *>(workspace);
+        d.t = static_cast<__bf16 *>(workspace) + kControlBytes / 2;
+        d.t_row = int32_t(t_row);
+        d.t_blocks = (runs.largest + kRanks - 1) / kRanks;
+        static std::atomic<uint64_t> attr_set{0};
+        const void *kern = reinterpret_cast<const void *>(&adapter_down_kernel);
+        int rc = allow_lds(kern, DownTile::kLds, dev, attr_set);
+        if (rc != LP_OK) return rc;
+        rc = lp::launch_kernel(kern, dim3(uint32_t(d.looks + runs.workgroups)), dim3(DownTile::kThreads), DownTile::kLds, stream, d);
+        if (rc != LP_OK) return rc;
+        a.control = d.control;
+        a.t = d.t;
+        a.t_row = d.t_row;
+        a.t_blocks = d.t_blocks;
+    }
+    a.runs = runs.runs;
+    for (int i = 0; i <= LP_MAX_REQUESTS; ++i) a.run[i] = runs.run[i];
+    const Plan p = pick_adapted(a.n, a.d_in, a.d_out, QKV ? HD : 0, cus, runs.runs, runs.run);
+    switch (p.tile * 8 + p.cut + 1) {
+        case 0 * 8 + 2: return launch_tiles<QKV, HD, Tile256x256, Tile256x128>(a, p.whole, stream);
+        case 0 * 8 + 3: return launch_tiles<QKV, HD, Tile256x256, Tile128x128>(a, p.whole, stream);
+        case 0 * 8 + 4: return launch_tiles<QKV, HD, Tile256x256, Tile128x64>(a, p.whole, stream);
+        case 2 * 8 + 4: return launch_tiles<QKV, HD, Tile128x128, Tile128x64>(a, p.whole, stream);
+        case 1 * 8: return launch_tiles<QKV, HD, Tile256x128, Tile256x128>(a, p.whole, stream);
+        case 2 * 8: return launch_tiles<QKV, HD, Tile128x128, Tile128x128>(a, p.whole, stream);
+        case 3 * 8: return launch_tiles<QKV, HD, Tile128x64, Tile128x64>(a, p.whole, stream);
+        default: return launch_tiles<QKV, HD, Tile256x256, Tile256x256>(a, p.whole, stream);
+    }
+}
+
+}  // namespace
+
+// For the tests, as lp_internal_gemm_way: rows and ranks of the requests.
+extern "C" int lp_internal_adapted_way(const int64_t *start, const int32_t *rank, int32_t count, int32_t d_in, int32_t d_out, int32_t head_dim,
+                                       int32_t cus, int64_t way[6]) {
+    AdapterRun run[LP_MAX_REQUESTS + 1];
+    int runs = 0;
+    for (int r = 0; r < count; ++r)
+        if (start[r + 1] > start[r]) run[runs++] = AdapterRun{int32_t(start[r]), rank[r], nullptr};
+    run[runs] = AdapterRun{int32_t(start[count]), 0, nullptr};
+    const int64_t n = start[count];
+    const Plan p = pick_adapted(int32_t(n), d_in, d_out, head_dim, cus, runs, run);
+    plan_way(p, n, d_out, false, way);
+    return LP_OK;
+}
+
+extern "C" int64_t lp_adapter_workspace_size(int64_t n_tokens, int32_t rank, int32_t sections) {
+    if (n_tokens < 0 || rank < 0 || (sections != 1 && sections != 3)) return LP_ERR_INVALID_ARG;
+    if (n_tokens >= INT32_MAX || rank > LP_MAX_ADAPTER_RANK) return LP_ERR_UNSUPPORTED;
+    return n_tokens > 0 && rank > 0 ? kControlBytes + n_tokens * t_row_bytes(rank, sections) : 0;
+}
+
+extern "C" int lp_linear_adapters(const void *x, const void *w, const float *bias, void *y, const lp_requests *requests, int32_t d_in,
+                                  int32_t d_out, const lp_adapter *adapters, void *workspace, int64_t workspace_bytes, void *stream) {
+    Runs runs;
+    int rc = make_runs(requests, adapters, d_in, d_out, 1, &runs);
+    if (rc != LP_OK) return rc;
+    const int64_t n = runs.requests.rows();
+    if ((rc = check_gemm_shape(n, d_in, d_out)) != LP_OK) return rc;
+    if (n == 0) return LP_OK;
+    if (runs.largest == 0) return lp_linear(x, w, bias, y, n, d_in, d_out, stream);
+    if (x == nullptr || w == nullptr || y == nullptr) return LP_ERR_INVALID_ARG;
+    if (!aligned16(x) || !aligned16(w) || !aligned16(y) || !aligned16(bias) || y == x || y == w) return LP_ERR_INVALID_ARG;
+    if (workspace == x || workspace == w || workspace == y) return LP_ERR_INVALID_ARG;
+    AdaptedArgs<false> a{};
+    a.x = static_cast<const __bf16 *>(x);
+    a.w = static_cast<const __bf16 *>(w);
+    a.bias = bias;
+    a.out[0] = static_cast<__bf16 *>(y);
+    a.n = int32_t(n);
+    a.d_in = d_in;
+    a.d_out = d_out;
+    return project<false, 128>(a, runs, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int lp_qkv_projection_adapters(const void *x, const void *w_qkv, const float *bias, const float *gain_q, const float *gain_k,
+                                          float eps, const lp_rope *ropes, void *q, void *k, void *v, const lp_requests *requests,
+                                          int32_t heads, int32_t head_dim, const lp_adapter *adapters, void *workspace,
+                                          int64_t workspace_bytes, void *stream) {
+    if (heads < 1) return LP_ERR_INVALID_ARG;
+    if (head_dim != 64 && head_dim != 128) return LP_ERR_UNSUPPORTED;
+    const int64_t dm64 = int64_t(heads) * head_dim;
+    if (3 * dm64 >= (int64_t(1) << 31)) return LP_ERR_UNSUPPORTED;
+    const int32_t dm = int32_t(dm64);
+    if (dm % 128 != 0) return LP_ERR_UNSUPPORTED;
+    Runs runs;
+    int rc = make_runs(requests, adapters, dm, 3 * dm, 3, &runs);
+    if (rc != LP_OK) return rc;
+    const int64_t n = runs.requests.rows();
+    if ((rc = check_gemm_shape(n, dm, 3 * dm)) != LP_OK) return rc;
+    if (n == 0) return LP_OK;
+    if (x == nullptr || w_qkv == nullptr || gain_q == nullptr || gain_k == nullptr || q == nullptr || k == nullptr || v == nullptr ||
+        ropes == nullptr)
+        return LP_ERR_INVALID_ARG;
+    if (!aligned16(x) || !aligned16(w_qkv) || !aligned16(bias) || !aligned16(gain_q) || !aligned16(gain_k) || !aligned16(q) ||
+        !aligned16(k) || !aligned16(v))
+        return LP_ERR_INVALID_ARG;
+    if (q == k || q == v || k == v || q == x || k == x || v == x) return LP_ERR_INVALID_ARG;
+    if (workspace != nullptr && (workspace == x || workspace == w_qkv || workspace == q || workspace == k || workspace == v)) return LP_ERR_INVALID_ARG;
+    AdaptedArgs<true> a{};
+    a.requests = runs.requests.count;
+    int first = -1;
+    for (int r = 0; r < a.requests; ++r) {
+        const int32_t start = runs.requests.start[r], rows = runs.requests.start[r + 1] - start;
+        a.grid[r] = RequestGrid{start, 1, 1, {0, 0, 0}};
+        if (rows == 0) continue;
+        if (first < 0) {
+            first = r;
+            if ((rc = make_rope_args(&ropes[r], rows, head_dim, eps, &a.rope)) != LP_OK) return rc;
+        }
+        RopeArgs unused;
+        const lp_rope &o = ropes[r];
+        if ((rc = make_rope_args(&o, rows, head_dim, eps, &unused)) != LP_OK) return rc;
+        if (o.base != ropes[first].base) return LP_ERR_INVALID_ARG;
+        for (int ax = 0; ax < 3; ++ax)
+            if (o.split[ax] != ropes[first].split[ax]) return LP_ERR_INVALID_ARG;
+        a.grid[r] = RequestGrid{start, o.grid[1] * o.grid[2], o.grid[2], {o.offset[0], o.offset[1], o.offset[2]}};
+    }
+    a.x = static_cast<const __bf16 *>(x);
+    a.w = static_cast<const __bf16 *>(w_qkv);
+    a.bias = bias;
+    a.out[0] = static_cast<__bf16 *>(q);
+    a.out[1] = static_cast<__bf16 *>(k);
+    a.out[2] = static_cast<__bf16 *>(v);
+    a.gain[0] = gain_q;
+    a.gain[1] = gain_k;
+    a.n = int32_t(n);
+    a.d_in = dm;
+    a.d_out = 3 * dm;
+    a.heads = heads;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return head_dim == 128 ? project<true, 128>(a, runs, workspace, workspace_bytes, st)
+                           : project<true, 64>(a, runs, workspace, workspace_bytes, st);
+}

@@ -72,14 +72,7 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(__bf16 *x, const float *
 
 extern "C" int lp_internal_gemm_way(int64_t n, int32_t d_in, int32_t d_out, int32_t head_dim, int32_t cus, int64_t way[6]) {
     const Plan p = pick_plan(n, d_in, d_out, small_tilings(head_dim), cus);
-    const TileCost &c = kTileCost[p.tile], &r = kTileCost[p.cut < 0 ? p.tile : p.cut];
-    const int64_t tiles = ((n + c.t - 1) / c.t) * ((d_out + c.f - 1) / c.f);
-    way[0] = c.f;
-    way[1] = c.t;
-    way[2] = p.cut < 0 ? 0 : r.f;
-    way[3] = p.cut < 0 ? 0 : r.t;
-    way[4] = p.whole + (tiles - p.whole) * (c.f / r.f) * (c.t / r.t);
-    way[5] = head_dim == 0 && four_waves(p, d_in) ? Wide256x256::kThreads : c.threads;
+    plan_way(p, n, d_out, head_dim == 0 && four_waves(p, d_in), way);
     return LP_OK;
 }
 

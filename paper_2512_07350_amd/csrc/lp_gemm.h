@@ -21,6 +21,7 @@
 #include <type_traits>
 
 #include "lp_device.h"
+#include "lp_requests.h"
 
 namespace {
 
@@ -51,6 +52,42 @@ struct GemmArgs {
     int32_t whole;               // workgroups [0, whole) take one tile each; the tiles from there on are cut in smaller ones
     RopeArgs rope;
 };
+
+// Low-rank adapters beside the product: y[i] += t[i] U_r^T for the rows i of run r (neighbouring requests with one adapter),
+// t[i] = s_r x[i] D_r^T computed beforehand (lp_adapters.hip).  The adapters are more k: behind the k-tiles of W and x a workgroup takes, for every
+// run that has rows in its tile and every 32 ranks, one k-tile whose W rows are U's and whose x rows are t's, zero outside the
+// run's rows.  t is held as a bf16 and the bf16 of what that leaves (2^-17 of the value together), as a k-tile of 64 holds 32 ranks of both: with
+// either beside the same columns of U, the only rounding to few bits is the result's.
+//
+// A row of another request meets U_r with zeros for t.  An infinity or a NaN in U_r would reach it all the same (0 x inf), so that
+// adapter_down_kernel has looked over every U_r: one that holds any is taken as zeros, and the t of its own rows as NaN.
+constexpr int kRanks = 32;               // ranks of a k-tile
+constexpr int kLooks = 16;               // words of a run that say whether parts of its U are not finite
+constexpr int kControlNan = 32;          // the control block in front of t: a k-tile's row of NaN, then kLooks words a run
+constexpr int kControlBytes = 4 * (kControlNan + LP_MAX_REQUESTS * kLooks);
+struct AdapterRun {
+    int32_t start, rank;                 // rows from start on, to the next run's; rank 0: no adapter
+    const __bf16 *up;                    // U [d_out, rank]
+};
+template <bool QKV>
+struct AdaptedArgs : GemmArgs {
+    // t: row i at i * t_row bytes, per section (q, k, v; one otherwise) t_blocks groups of 32 ranks: 32 values, then what they leave
+    const __bf16 *t;
+    const uint32_t *control;
+    int32_t t_row, t_blocks, runs;
+    AdapterRun run[LP_MAX_REQUESTS + 1];         // entries past the last start behind every row
+};
+// QKV: where the tokens of each request are rotated to.
+struct RequestGrid {
+    int32_t start, hw, w, off[3];
+};
+template <>
+struct AdaptedArgs<true> : AdaptedArgs<false> {
+    int32_t requests;
+    RequestGrid grid[LP_MAX_REQUESTS];
+};
+template <typename Args>
+constexpr bool kAdapted = std::is_base_of<AdaptedArgs<false>, Args>::value;
 
 // granule XOR mask of a tile row (reader and writer use the same function): with 128-byte rows
 // the 16-byte granule g of row r lives at position g ^ swz(r), which makes the ds_read_b128 of
@@ -101,6 +138,103 @@ struct Tiling {
     static_assert(kWaves % 2 == 0 && kF % (16 * kWaves) == 0 && (kT % (8 * kWaves) == 0 || TB == 1) && FB % 2 == 0, "whole loads");
 };
 
+// The k-tiles of the adapters of one tile: kF features from f0 on, kT tokens from t0 on.  Everything is the same in all lanes
+// (scalar registers) but the offsets of a load.
+template <typename C, typename Args>
+struct AdapterTiles {
+    static constexpr bool QKV = std::is_same<Args, AdaptedArgs<true>>::value;
+    const Args &a;
+    const int f0, t0;
+    uint64_t left = 0;                   // runs still to come, the present one included
+    int count = 0;                       // k-tiles in all
+    int first_section, last_section;
+    // the present one
+    int section = 0, block = 0, blocks = 0;
+    uint32_t granules = 0, t_col = 0;    // 16-byte pieces of U's rows; offset of the k-tile in t's
+    uint32_t t_row = 0;                  // bytes from row to row of t; 0: every row is the one of NaN, U is zeros
+    int t_lo = 0, t_hi = 0, f_lo = 0, f_hi = 0;          // rows of the tile that are the run's, features that are the section's
+    __amdgpu_buffer_rsrc_t u_rsrc, t_rsrc;
+
+    __device__ __forceinline__ AdapterTiles(const Args &args, int f, int t, int lane) : a(args), f0(f), t0(t) {
+        const int dm = QKV ? a.d_out / 3 : a.d_out;
+        first_section = f0 / dm;
+        last_section = min(f0 + C::kF - 1, a.d_out - 1) / dm;
+        const int32_t start = a.run[lane].start, end = a.run[lane + 1].start, rank = a.run[lane].rank;
+        const int of_run = rank > 0 && start - t0 < C::kT && end > t0 ? (rank + kRanks - 1) / kRanks : 0;
+        left = __ballot(of_run > 0);
+        for (uint64_t m = left; m != 0; m &= m - 1) count += __builtin_amdgcn_readlane(of_run, __builtin_ctzll(m));
+        count *= last_section - first_section + 1;
+        section = last_section;          // next() turns to the first run
+        u_rsrc = t_rsrc = buffer(a.t, 0);
+    }
+    __device__ __forceinline__ static __amdgpu_buffer_rsrc_t buffer(const void *p, int64_t bytes) {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, int(bytes), 0x00020000);
+    }
+    // Scalar loads: a vector load would be waited for behind all that is on its way to LDS.
+    __device__ __forceinline__ bool not_finite(int r) const {
+        typedef __attribute__((address_space(4))) const uint32_t Words;
+        Words *w = (Words *)(uintptr_t(a.control + kControlNan + r * kLooks));
+        uint32_t any = 0;
+#pragma unroll
+        for (int i = 0; i < kLooks; ++i) any |= w[i];
+        return any != 0;
+    }
+    // The k-tile behind the present one.  Past the last one: one of zeros.
+    __device__ __forceinline__ void next() {
+        if (++block < blocks) {
+            t_col += t_row != 0 ? 4 * kRanks : 0;
+            return;
+        }
+        if (blocks > 0 && section == last_section) left &= left - 1;
+        if (left == 0) {
+            t_hi = f_hi = 0;
+            granules = 0;
+            return;
+        }
+        section = section == last_section ? first_section : section + 1;
+        const int r = __builtin_ctzll(left);
+        const int rank = a.run[r].rank;
+        blocks = (rank + kRanks - 1) / kRanks;
+        block = 0;
+        granules = uint32_t(rank) / 8;
+        t_lo = max(a.run[r].start - t0, 0);
+        t_hi = min(a.run[r + 1].start - t0, C::kT);
+        const int dm = QKV ? a.d_out / 3 : a.d_out;
+        f_lo = section * dm - f0;
+        f_hi = f_lo + dm;
+        const int64_t t_rows = min(int64_t(C::kT), int64_t(a.n) - t0), u_rows = min(int64_t(C::kF), int64_t(a.d_out) - f0);
+        if (not_finite(r)) {
+            t_row = t_col = 0;
+            t_rsrc = buffer(a.control, 4 * kRanks);
+            u_rsrc = buffer(a.run[r].up, 0);
+        } else {
+            t_row = uint32_t(a.t_row);
+            t_col = uint32_t(section) * uint32_t(a.t_blocks) * (4 * kRanks);
+            t_rsrc = buffer(reinterpret_cast<const unsigned char *>(a.t) + int64_t(t0) * a.t_row, t_rows * a.t_row);
+            u_rsrc = buffer(a.run[r].up + int64_t(f0) * rank, u_rows * rank * 2);
+        }
+    }
+    // Where lane `lane` of a load of rows 8 group .. 8 group + 7 fetches its granule g (0 .. 7) from; out of the buffer: zeros
+    __device__ __forceinline__ uint32_t t_offset(int group, int lane, uint32_t g) const {
+        const int row = 8 * group + lane / 8;
+        const bool in = row >= t_lo && row < t_hi && uint32_t(block) * 4 + g % 4 < granules;
+        return in ? uint32_t(row) * t_row + t_col + 16 * g : 0x80000000u;
+    }
+    __device__ __forceinline__ uint32_t u_offset(int group, int lane, uint32_t g) const {
+        const int row = 8 * group + lane / 8;
+        const uint32_t piece = uint32_t(block) * 4 + g % 4;
+        return row >= f_lo && row < f_hi && piece < granules ? (uint32_t(row) * granules + piece) * 16 : 0x80000000u;
+    }
+};
+// What a product without adapters has instead.
+struct NoAdapterTiles {
+    static constexpr int count = 0;
+    template <typename Args>
+    __device__ __forceinline__ NoAdapterTiles(const Args &, int, int, int) {}
+};
+template <typename C, typename Args>
+using AdapterTilesOf = std::conditional_t<kAdapted<Args>, AdapterTiles<C, Args>, NoAdapterTiles>;
+
 // acc[f][t] += W[f0 + ..] . x[t0 + ..]^T over all of k.
 //
 // What bounds it.  A k-tile is kStage bytes arriving in LDS against 2 kF kT 64 flop.  With a stage
@@ -115,8 +249,8 @@ struct Tiling {
 // 1131 -> 1380 TFLOP/s (32x32x16 products: 1312; 256 x 256 tile, back to back on one box); matrix pipeline busy
 // 76 % of the cycles, at a clock that the power limit holds to 1.65 GHz.  Among other kernels, with its epilogue, the
 // projection runs at 1050 to 1370 by the clock the card has at the time (1.98 to 1.52 ms, 1.76 on average).
-template <typename C>
-__device__ __forceinline__ void product(uint32_t lds0, const GemmArgs &a, int f0, int t0, int wave, int lane,
+template <typename C, typename Args>
+__device__ __forceinline__ void product(uint32_t lds0, const Args &a, int f0, int t0, int wave, int lane,
                                         f32x4 (&acc)[C::FB][C::TB]) {
     constexpr int FB = C::FB, TB = C::TB, FH = C::FH, S = C::S, W = C::kWaves;
     const int col = lane % 16, quad = lane / 16;
@@ -144,6 +278,21 @@ __device__ __forceinline__ void product(uint32_t lds0, const GemmArgs &a, int f0
         else load(w_rsrc, lo_group(i - C::kLoadsX), kt, stage);
     };
     auto load_y = [&](int i, int kt, uint32_t stage) { load(w_rsrc, lo_group(i) + kHalfGroups, kt, stage); };
+    // the same for the present k-tile of the adapters
+    AdapterTilesOf<C, Args> extra(a, f0, t0, lane);
+    const uint32_t granule = (lane % 8) ^ swz((wave & 1) * 8 + lane / 8);
+    auto load_u = [&](int group, uint32_t stage) {
+        if constexpr (kAdapted<Args>)
+            load_to_lds_16(extra.u_rsrc, __builtin_amdgcn_readfirstlane(lds0 + stage + group * 1024), extra.u_offset(group, lane, granule), 0);
+    };
+    auto load_extra_x = [&](int i, uint32_t stage) {
+        if constexpr (kAdapted<Args>) {
+            if (i >= C::kLoadsX) return load_u(lo_group(i - C::kLoadsX), stage);
+            const int group = wave + i * W;
+            load_to_lds_16(extra.t_rsrc, __builtin_amdgcn_readfirstlane(lds0 + stage + C::kWBytes + group * 1024), extra.t_offset(group, lane, granule), 0);
+        }
+    };
+    auto load_extra_y = [&](int i, uint32_t stage) { load_u(lo_group(i) + kHalfGroups, stage); };
 
     // operand addresses of the two k-steps of 32 in the stage being read
     uint32_t w_addr[2], x_addr[2];
@@ -157,14 +306,22 @@ __device__ __forceinline__ void product(uint32_t lds0, const GemmArgs &a, int f0
     auto read_hi = [&](int m, int s) { hi[m][s] = lds_load<bf16x8>(w_addr[s] + (FH + m) * 16 * kRowBytes); };
     auto read_x = [&](int t, int s) { xop[t][s] = lds_load<bf16x8>(x_addr[s] + t * 16 * kRowBytes); };
 
-    const int n_kt = a.d_in / kBK;
+    const int n_plain = a.d_in / kBK, n_kt = n_plain + extra.count;
 #pragma unroll
     for (int p = 0; p < S; ++p) {
-        if (p < n_kt) {
+        if (p < n_plain) {
 #pragma unroll
             for (int i = 0; i < C::X; ++i) load_x(i, p, p * C::kStage);
 #pragma unroll
             for (int i = 0; i < C::Y; ++i) load_y(i, p, p * C::kStage);
+        } else if constexpr (kAdapted<Args>) {
+            if (p < n_kt) {
+                extra.next();
+#pragma unroll
+                for (int i = 0; i < C::X; ++i) load_extra_x(i, p * C::kStage);
+#pragma unroll
+                for (int i = 0; i < C::Y; ++i) load_extra_y(i, p * C::kStage);
+            }
         }
     }
     // in registers from here on: zeroed right in front of the first products they would be read a wait state too early
@@ -187,8 +344,9 @@ __device__ __forceinline__ void product(uint32_t lds0, const GemmArgs &a, int f0
     static_assert(PRE >= 1 && PRE < PK, "the lo operands are read between the barrier and the k-step's end");
     uint32_t cur = 0;                                    // stage of tile kt
     // LEFT = tiles after this one, as far as the code depends on it: with LEFT = S there is also a tile
-    // to send for (kt + S); below that everything that is left is already under way.
-    auto tile = [&](int kt, auto left_c) {
+    // to send for (kt + S, EXTRA: one of the adapters); below that everything that is left is already under way.
+    auto tile = [&](int kt, auto left_c, auto extra_c) {
+        constexpr bool EXTRA = decltype(extra_c)::value;
         constexpr int LEFT = decltype(left_c)::value;
         constexpr bool REFILL = LEFT >= S;
         constexpr int AHEAD = REFILL ? S - 1 : LEFT;     // later tiles whose loads are under way
@@ -213,7 +371,10 @@ __device__ __forceinline__ void product(uint32_t lds0, const GemmArgs &a, int f0
                         read_hi(r % FH, r / FH);
                     });
                 if constexpr (REFILL)
-                    static_for<j * C::X / rest, (j + 1) * C::X / rest>([&](auto rc) { load_x(decltype(rc)::value, kt + S, cur); });
+                    static_for<j * C::X / rest, (j + 1) * C::X / rest>([&](auto rc) {
+                        if constexpr (EXTRA) load_extra_x(decltype(rc)::value, cur);
+                        else load_x(decltype(rc)::value, kt + S, cur);
+                    });
             }
         });
         // ---- phase 2: hi x x; meanwhile the first k-step of the next tile's lo and x operands
@@ -239,17 +400,25 @@ __device__ __forceinline__ void product(uint32_t lds0, const GemmArgs &a, int f0
                 }
                 if constexpr (REFILL && i >= PRE) {
                     constexpr int j = i - PRE, rest = 2 * PK - PRE;
-                    static_for<j * C::Y / rest, (j + 1) * C::Y / rest>([&](auto rc) { load_y(decltype(rc)::value, kt + S, cur); });
+                    static_for<j * C::Y / rest, (j + 1) * C::Y / rest>([&](auto rc) {
+                        if constexpr (EXTRA) load_extra_y(decltype(rc)::value, cur);
+                        else load_y(decltype(rc)::value, kt + S, cur);
+                    });
                 }
             }
         });
         cur = nxt;
     };
     int kt = 0;
-    for (; kt + S < n_kt; ++kt) tile(kt, std::integral_constant<int, S>{});
+    for (; kt + S < n_plain; ++kt) tile(kt, std::integral_constant<int, S>{}, std::false_type{});
+    if constexpr (kAdapted<Args>)
+        for (; kt + S < n_kt; ++kt) {
+            extra.next();
+            tile(kt, std::integral_constant<int, S>{}, std::true_type{});
+        }
     static_for<0, S>([&](auto lc) {
         constexpr int LEFT = S - 1 - decltype(lc)::value;
-        if (kt + LEFT == n_kt - 1) tile(kt++, std::integral_constant<int, LEFT>{});
+        if (kt + LEFT == n_kt - 1) tile(kt++, std::integral_constant<int, LEFT>{}, std::false_type{});
     });
     // products become readable by vector instructions
     asm volatile("s_nop 15\n\ts_nop 7");
@@ -498,23 +667,46 @@ __device__ __forceinline__ void product_split_k(uint32_t lds0, const GemmArgs &a
         }
 }
 
+// Coordinates of token tk in its request's grid; the lanes' tokens lie between `first` and `last`, mostly of one request.
+__device__ __forceinline__ void grid_position(const AdaptedArgs<true> &a, int32_t tk, int32_t first, int32_t last, float &t, float &h, float &w) {
+    const int lane = threadIdx.x % 64;
+    const int32_t start = lane < a.requests ? a.grid[lane].start : INT32_MAX;
+    int r = __popcll(__ballot(start <= first)) - 1;
+    const int end = __popcll(__ballot(start <= last)) - 1;
+    RequestGrid g = a.grid[r];
+    while (r < end) {                                    // the later requests, those without rows included, which the next one replaces
+        ++r;
+        const RequestGrid &o = a.grid[r];
+        if (tk >= o.start) g = o;
+    }
+    const uint32_t local = uint32_t(tk - g.start), ct = local / uint32_t(g.hw), rem = local - ct * uint32_t(g.hw), ch = rem / uint32_t(g.w);
+    t = float(int32_t(ct) + g.off[0]);
+    h = float(int32_t(ch) + g.off[1]);
+    w = float(int32_t(rem - ch * uint32_t(g.w)) + g.off[2]);
+}
+
 // Per-head RMS normalisation and rotary encoding, in place, of the features a wave holds in acc
 // (those of one section of q or k): block f, token block t, element i of lane (col, quad) is
 // feature 16 f + 4 quad + i of token 16 t + col.  sum_sq(t, h) is the sum of squares over the
 // h-th head's features; gain_lds holds the gains of the wave's features; in_head is the first one's
 // place in its head.  The rotary table sits in LDS at rope_lds, float4 per pair.
-template <int HD, typename C, typename F>
+template <int HD, typename C, typename F, typename Args>
 __device__ __forceinline__ void norm_rope(f32x4 (&acc)[C::FB][C::TB], F &&sum_sq, uint32_t gain_lds, int in_head,
-                                          const RopeArgs &r, uint32_t rope_lds, int tok_first, int n, int col, int quad) {
+                                          const Args &a, uint32_t rope_lds, int tok_first, int col, int quad) {
+    const RopeArgs &r = a.rope;
     constexpr int kHeads = C::FB * 16 > HD ? C::FB * 16 / HD : 1, kBlocks = C::FB / kHeads;
     float pt[C::TB], ph[C::TB], pw[C::TB];               // coordinates of this lane's tokens
 #pragma unroll
     for (int t = 0; t < C::TB; ++t) {
-        const uint32_t tk = uint32_t(min(tok_first + 16 * t + col, n - 1));
-        const uint32_t ct = fastdiv(tk, r.hw), rem = tk - ct * r.hw.d, ch = fastdiv(rem, r.w);
-        pt[t] = float(int32_t(ct) + r.off[0]);
-        ph[t] = float(int32_t(ch) + r.off[1]);
-        pw[t] = float(int32_t(rem - ch * r.w.d) + r.off[2]);
+        const uint32_t tk = uint32_t(min(tok_first + 16 * t + col, a.n - 1));
+        if constexpr (kAdapted<Args>) {
+            grid_position(a, int32_t(tk), min(tok_first + 16 * t, a.n - 1), min(tok_first + 16 * t + 15, a.n - 1), pt[t], ph[t], pw[t]);
+        } else {
+            const uint32_t ct = fastdiv(tk, r.hw), rem = tk - ct * r.hw.d, ch = fastdiv(rem, r.w);
+            pt[t] = float(int32_t(ct) + r.off[0]);
+            ph[t] = float(int32_t(ch) + r.off[1]);
+            pw[t] = float(int32_t(rem - ch * r.w.d) + r.off[2]);
+        }
     }
 #pragma unroll
     for (int hh = 0; hh < kHeads; ++hh) {
@@ -572,8 +764,8 @@ __device__ __forceinline__ void store_tile(uint32_t out_lds, const f32x4 (&acc)[
 
 // One tile from its first load to its last store.  QKV = true: the epilogue cuts the features into
 // q | k | v sections of heads * HD, normalises and rotates q and k.  QKV = false: plain y = x W^T + b.
-template <bool QKV, int HD, typename C>
-__device__ __forceinline__ void run_tile(uint32_t lds0, const GemmArgs &a, int f0, int t0) {
+template <bool QKV, int HD, typename C, typename Args>
+__device__ __forceinline__ void run_tile(uint32_t lds0, const Args &a, int f0, int t0) {
     constexpr int FB = C::FB, TB = C::TB;
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
@@ -593,6 +785,7 @@ __device__ __forceinline__ void run_tile(uint32_t lds0, const GemmArgs &a, int f
         const float *tp = a.rope.turns[tid % kMaxPairs];
         turns_pre = f32x4{tp[0], tp[1], tp[2], 0.0f};
     }
+    static_assert(!kAdapted<Args> || C::HOW == kShared, "the others know nothing of adapters");
     f32x4 acc[FB][TB];
     if constexpr (C::SPLIT) product_split_k<C>(lds0, a, f0, t0, wave, lane, acc);
     else if constexpr (C::HOW == kWide) product_wide<C>(lds0, a, f0, t0, wave, lane, acc);
@@ -627,7 +820,7 @@ __device__ __forceinline__ void run_tile(uint32_t lds0, const GemmArgs &a, int f
             for (int i = 0; i < 4; ++i) acc[f][t][i] += b4[i];
     }
     const int tok_first = t0 + (wave % C::WT) * TB * 16;
-    if (QKV) {
+    if constexpr (QKV) {
         // sums of squares over the features of a head that this wave holds
         constexpr int kHeads = FB * 16 > HD ? FB * 16 / HD : 1, kSharing = FB * 16 < HD ? HD / (FB * 16) : 1;
         float ss[TB][kHeads];
@@ -663,8 +856,8 @@ __device__ __forceinline__ void run_tile(uint32_t lds0, const GemmArgs &a, int f
             }
         }
         if (section < 2)
-            norm_rope<HD, C>(acc, [&](int t, int hh) { return ss[t][hh]; }, gain_lds, f_in_section % HD, a.rope, rope_lds, tok_first,
-                             a.n, col, quad);
+            norm_rope<HD, C>(acc, [&](int t, int hh) { return ss[t][hh]; }, gain_lds, f_in_section % HD, a, rope_lds, tok_first, col,
+                             quad);
     } else if (!live) {
         return;
     }
@@ -674,8 +867,8 @@ __device__ __forceinline__ void run_tile(uint32_t lds0, const GemmArgs &a, int f
 // Workgroups [0, whole) take one tile of tiling P each; every later tile is cut into tiles of R.
 // P's tiles are ordered in panels of kPanel token tiles, feature tile by feature tile inside a
 // panel: the workgroups an XCD runs at a time share their W and x rows through its L2.
-template <bool QKV, int HD, typename P, typename R>
-__global__ __launch_bounds__(P::kThreads, P::HOW == kShared ? 2 : 1) void gemm_kernel(const GemmArgs a) {
+template <bool QKV, int HD, typename P, typename R, typename Args>
+__global__ __launch_bounds__(P::kThreads, P::HOW == kShared ? 2 : 1) void gemm_kernel(const Args a) {
     static_assert(P::kThreads == R::kThreads && P::kF % R::kF == 0 && P::kT % R::kT == 0, "R cuts P");
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const uint32_t lds0 = uint32_t(uintptr_t(LP_LDS_PTR(unsigned char, smem)));
@@ -797,9 +990,11 @@ struct Plan {
 // longer (24000 x 256 -> 5120: 87 us whole, 106 cut), so that a cut has to promise 5 % there.
 // One round of 120 to 250 tiles of 128 x 64 is faster than one of half as many of 128 x 128: 1271 x 704 -> 1536 6.7 and 8.1 us.
 // Over the calls above the choice is off the best tiling by 0.4 % on average, by more than 10 % in 20 of them.
-Plan pick_plan(int64_t n, int32_t d_in, int32_t d_out, bool small_ok, int cus) {
+//
+// k_tiles(t): k-tiles of a tile of t tokens, on average.
+template <typename F>
+Plan pick_plan(int64_t n, int32_t d_out, bool small_ok, int cus, F &&k_tiles) {
     static constexpr int kCuts[][2] = {{0, 1}, {0, 2}, {0, 3}, {2, 3}};   // the pairs compiled below
-    const int n_kt = d_in / kBK;
     auto count = [&](int k) { return ((n + kTileCost[k].t - 1) / kTileCost[k].t) * ((d_out + kTileCost[k].f - 1) / kTileCost[k].f); };
     Plan best{0, kCutNone, 0};
     float best_us = 0.0f;
@@ -809,23 +1004,27 @@ Plan pick_plan(int64_t n, int32_t d_in, int32_t d_out, bool small_ok, int cus) {
         best = Plan{tile, cut, whole};
         best_us = us;
     };
-    for (int k = 0; k < (small_ok ? 6 : 4); ++k) offer(k, kCutNone, count(k), count(k), tiles_cost(kTileCost[k], count(k), n_kt, cus));
+    for (int k = 0; k < (small_ok ? 6 : 4); ++k)
+        offer(k, kCutNone, count(k), count(k), tiles_cost(kTileCost[k], count(k), k_tiles(kTileCost[k].t), cus));
     for (const auto &p : kCuts) {
         const TileCost &big = kTileCost[p[0]], &small = kTileCost[p[1]];
         const int64_t tiles = count(p[0]), whole = tiles / cus * cus;
         if (whole == 0 || whole == tiles) continue;
         const int64_t parts = (tiles - whole) * (big.f / small.f) * (big.t / small.t);
-        const float cut_us = tiles_cost(big, whole, n_kt, cus) + tiles_cost(small, parts, n_kt, cus);
-        offer(p[0], p[1], whole, whole + parts, n_kt < 12 ? 1.05f * cut_us : cut_us);
+        const float cut_us = tiles_cost(big, whole, k_tiles(big.t), cus) + tiles_cost(small, parts, k_tiles(small.t), cus);
+        offer(p[0], p[1], whole, whole + parts, k_tiles(big.t) < 12 ? 1.05f * cut_us : cut_us);
     }
     return best;
 }
+Plan pick_plan(int64_t n, int32_t d_in, int32_t d_out, bool small_ok, int cus) {
+    return pick_plan(n, d_out, small_ok, cus, [d_in](int) { return d_in / kBK; });
+}
 
-template <bool QKV, int HD, typename P, typename R>
-int launch_tiles(GemmArgs a, int64_t whole, hipStream_t stream) {
+template <bool QKV, int HD, typename P, typename R, typename Args>
+int launch_tiles(Args a, int64_t whole, hipStream_t stream) {
     constexpr int kLds = P::kLds > R::kLds ? P::kLds : R::kLds;
     static std::atomic<uint64_t> attr_set{0};
-    const void *kern = reinterpret_cast<const void *>(&gemm_kernel<QKV, HD, P, R>);
+    const void *kern = reinterpret_cast<const void *>(&gemm_kernel<QKV, HD, P, R, Args>);
     int dev = 0;
     const hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) {
@@ -883,6 +1082,18 @@ int launch_gemm(GemmArgs a, hipStream_t stream) {
             [[fallthrough]];
         default: return launch_tiles<QKV, HD, Tile256x256, Tile256x256>(a, p.whole, stream);
     }
+}
+
+// A plan as lp_internal_gemm_way states it.
+void plan_way(const Plan &p, int64_t n, int32_t d_out, bool four, int64_t way[6]) {
+    const TileCost &c = kTileCost[p.tile], &r = kTileCost[p.cut < 0 ? p.tile : p.cut];
+    const int64_t tiles = ((n + c.t - 1) / c.t) * ((d_out + c.f - 1) / c.f);
+    way[0] = c.f;
+    way[1] = c.t;
+    way[2] = p.cut < 0 ? 0 : r.f;
+    way[3] = p.cut < 0 ? 0 : r.t;
+    way[4] = p.whole + (tiles - p.whole) * (c.f / r.f) * (c.t / r.t);
+    way[5] = four ? Wide256x256::kThreads : c.threads;
 }
 
 // shape limits of the product: k in whole tiles, 32-bit byte offsets inside a tile's rows

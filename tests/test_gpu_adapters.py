@@ -1,0 +1,371 @@
+"""lp_linear_adapters and lp_qkv_projection_adapters against the definition in 64 bits.
+
+Tolerance.  Sums of bf16 products are formed in binary32, at most d_in / 32 + 2 rank / 32 of them one after the other with a few
+roundings around (bias, wavefronts' parts): c = (d_in / 32 + rank / 16 + 24) 2^-24 of the sum of magnitudes.  t = s D x carries the same error, and
+2^-17 of itself as two bf16.  So a projection is off by
+    c (|W| |x| + |b| + s |U| |D| |x|) + 2^-17 |U| |t|,
+formed element by element below, and by 2^-8 of the result when it is rounded.  A head that is normalised multiplies this by gain / rms, once for the
+element and once, through the rms, for all of them (at most the largest of them times |v|); a rotation adds what both elements of a pair are off by,
+and angles of p radians in binary32 turns are off by (p + 1) 2^-21 with the hardware's sine and cosine (2^-18) behind them.
+"""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+from paper_2512_07350_amd import binding as lp
+from tests import routes
+
+pytestmark = pytest.mark.gpu
+
+EPS = 1e-6
+
+
+def way(lengths, ranks, d_in, d_out, head_dim=0):
+    """What a call runs: routes.GemmWay."""
+    fn = lp._lib().lp_internal_adapted_way
+    fn.argtypes = [C.POINTER(C.c_int64), C.POINTER(C.c_int32), C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int64)]
+    starts = np.concatenate([[0], np.cumsum(lengths)]).tolist()
+    out = (C.c_int64 * 6)()
+    assert fn((C.c_int64 * len(starts))(*starts), (C.c_int32 * len(ranks))(*ranks), len(ranks), d_in, d_out, head_dim, routes._cus(None), out) == 0
+    return routes.GemmWay((out[0], out[1]), (out[2], out[3]) if out[2] else None, out[4], out[5])
+
+
+class Case:
+    def __init__(self, lengths, ranks, d_in, d_out, sections=1, bias=True, seed=1, up=0.2, own=True, x_scale=1.0):
+        import torch
+        self.lengths, self.ranks, self.d_in, self.d_out, self.sections = list(lengths), list(ranks), d_in, d_out, sections
+        self.starts = np.concatenate([[0], np.cumsum(lengths)]).tolist()
+        self.n = self.starts[-1]
+        gen = torch.Generator(device="cuda").manual_seed(9000 + 7 * seed + self.n)
+        f = lambda *shape: torch.randn(shape, generator=gen, device="cuda", dtype=torch.float32)
+        bf = lambda t: t.to(torch.bfloat16)
+        self.x = bf(x_scale * f(self.n, d_in))
+        self.w = bf(f(d_out, d_in) * d_in ** -0.5)
+        self.bias = 0.5 * f(d_out) if bias else None
+        self.adapters = [(bf(f(sections * r, d_in) * d_in ** -0.5), bf(up * f(d_out, r)), 0.75 + 0.25 * i) if r else None
+                         for i, r in enumerate(self.ranks)]
+
+    def workspace(self, extra=0):
+        import torch
+        size = lp.lp_adapter_workspace_size(self.n, max(self.ranks), self.sections)
+        # NaN everywhere: what no one wrote in this call shows
+        return torch.full((size // 2 + 64 + extra,), float("nan"), dtype=torch.bfloat16, device="cuda"), size
+
+    def want(self, rows=slice(None)):
+        """(projection in 64 bits, what binary32 may be off by) of the rows."""
+        import torch
+        c = (self.d_in / 32 + max(self.ranks) / 16 + 24) * 2.0 ** -24
+        index = torch.arange(self.n, device="cuda")[rows]
+        x, w = self.x[index].double(), self.w.double()
+        y = x @ w.t()
+        off = c * (x.abs() @ w.abs().t())
+        if self.bias is not None:
+            y += self.bias.double()
+            off += c * self.bias.double().abs()
+        part = self.d_out // self.sections
+        for r, ad in enumerate(self.adapters):
+            here = (index >= self.starts[r]) & (index < self.starts[r + 1])
+            if ad is None or not bool(here.any()):
+                continue
+            down, up, scale = ad[0].double(), ad[1].double(), float(np.float32(ad[2]))
+            rank = up.shape[1]
+            t, ta = scale * (x[here] @ down.t()), scale * (x[here].abs() @ down.abs().t())
+            for s in range(self.sections):
+                cols, k = slice(s * part, (s + 1) * part), slice(s * rank, (s + 1) * rank)
+                y[here, cols] += t[:, k] @ up[cols].t()
+                off[here, cols] += (c * ta[:, k] + 2.0 ** -17 * t[:, k].abs()) @ up[cols].abs().t() + c * (ta[:, k] @ up[cols].abs().t())
+        return y, off
+
+    def linear(self, extra=3):
+        import torch
+        y = torch.full((self.n + extra, self.d_out), 77.0, dtype=torch.bfloat16, device="cuda")
+        ws, size = self.workspace()
+        lp.lp_linear_adapters(self.x, self.w, self.bias, y, lp.make_requests(self.starts), self.d_in, self.d_out, lp.make_adapters(self.adapters), ws, size,
+                              torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        assert torch.isnan(ws[size // 2:].float()).all()
+        assert (y[self.n:] == 77.0).all()
+        return y[:self.n]
+
+
+def inside(got, want, off, what=""):
+    import torch
+    assert got.shape == want.shape and torch.isfinite(got.float()).all(), what
+    excess = (got.double() - want).abs() - (off + 2.0 ** -8 * (want.abs() + off))
+    assert float(excess.max()) <= 0, (what, float(excess.max()), divmod(int(excess.argmax()), want.shape[-1]))
+
+
+# one token to several tiles, requests that share tiles, without rows, without adapters, ranks of part of a k-tile, one and several, k of
+# fewer k-tiles than stages
+@pytest.mark.parametrize("lengths,ranks,d_in,d_out", [
+    ([1], [8], 64, 128), ([1, 1, 1], [8, 0, 40], 64, 384), ([5, 0, 12, 3], [16, 24, 0, 64], 128, 256), ([33, 31], [32, 256], 192, 128),
+    ([64, 64, 64], [8, 16, 32], 320, 640), ([130, 1, 127, 300], [72, 8, 136, 0], 448, 1152), ([1] * 64, [8 * (1 + i % 5) for i in range(64)], 512, 512),
+    ([257, 255, 1], [128, 0, 96], 1536, 1536), ([520], [64], 5120, 640), ([700, 800], [48, 200], 2112, 1408),
+])
+def test_linear_adapters(lengths, ranks, d_in, d_out):
+    for bias in (True, False):
+        c = Case(lengths, ranks, d_in, d_out, bias=bias)
+        inside(c.linear(), *c.want(), (lengths, ranks))
+
+
+TILINGS = [
+    (66, 64, 8448, "128x64"), (1438, 1024, 1152, "128x64"), (1345, 576, 1536, "128x128"), (75077, 64, 128, "128x128+128x64"),
+    (12001, 1024, 384, "256x128"), (3783, 128, 3840, "256x256"), (3600, 128, 4608, "256x256+128x64"), (4097, 1024, 4608, "256x256+128x128"),
+    (3601, 512, 6144, "256x256+256x128"),
+]
+
+
+@pytest.mark.parametrize("n,d_in,d_out,tiles", TILINGS)
+def test_linear_adapters_of_every_tiling(n, d_in, d_out, tiles):
+    """Four requests whose edges lie inside tiles, one in the middle without adapter."""
+    lengths = [n // 3 + 5, n // 4, n // 5, 0]
+    lengths[3] = n - sum(lengths)
+    ranks = [32, 0, 16, 32]
+    assert str(way(lengths, ranks, d_in, d_out)) == tiles
+    c = Case(lengths, ranks, d_in, d_out)
+    y = c.linear()
+    edges = [s + i for s in c.starts for i in (-2, -1, 0, 1) if 0 <= s + i < n]
+    import torch
+    rows = torch.tensor(sorted(set(edges + list(range(0, n, max(1, n // 400))) + list(range(min(n, 40))))), device="cuda")
+    inside(y[rows], *c.want(rows), tiles)
+    assert torch.isfinite(y.float()).all()
+
+
+def test_large_adapters_beside_small_weights():
+    """The adapter's part a hundred times the projection's: t keeps 17 bits."""
+    c = Case([300, 50], [64, 16], 512, 256, up=20.0)
+    inside(c.linear(), *c.want())
+
+
+def test_neighbours_with_one_adapter_are_one_run():
+    import torch
+    c = Case([200, 0, 311, 77], [32, 16, 32, 0], 256, 384)
+    c.adapters[2] = c.adapters[0]
+    a = c.linear()
+    inside(a, *c.want())
+    joined = Case([511, 77], [32, 0], 256, 384)
+    joined.x, joined.w, joined.bias, joined.adapters = c.x, c.w, c.bias, [c.adapters[0], None]
+    assert torch.equal(a, joined.linear())
+
+
+def test_requests_without_adapters_are_the_plain_projection():
+    import torch
+    c = Case([300, 220], [0, 0], 1536, 1536)
+    y = c.linear()
+    plain = torch.empty_like(y)
+    lp.lp_linear(c.x, c.w, c.bias, plain, c.n, c.d_in, c.d_out, torch.cuda.current_stream().cuda_stream)
+    assert torch.equal(y, plain)
+
+
+def test_a_request_of_nan_leaves_the_others_alone():
+    """NaN and infinities in one request's rows and in its adapter."""
+    import torch
+    c = Case([70, 30, 60], [32, 40, 16], 256, 256)
+    c.x[75, 3] = float("nan")
+    c.x[80] = float("inf")
+    c.adapters[1][1][5, 7] = float("inf")
+    y = c.linear()
+    for rows in (slice(0, 70), slice(100, 160)):
+        inside(y[rows], *c.want(rows))
+    assert torch.isnan(y[70:100].float()).all()            # what is said of an adapter that is not finite: not taken for zeros
+
+
+@pytest.mark.parametrize("at", [0, 1, 1000, 81919, 2 ** 19 + 4, 5120 * 256 - 1])
+def test_every_part_of_an_adapter_is_looked_over(at):
+    import torch
+    c = Case([20, 20, 9], [8, 256, 256], 64, 5120)
+    c.adapters[1][1].view(-1)[at] = float("-inf")
+    y = c.linear()
+    inside(y[:20], *c.want(slice(0, 20)))
+    inside(y[40:], *c.want(slice(40, 49)))
+    assert torch.isnan(y[20:40].float()).all()
+
+
+# ---- q | k | v
+
+class Qkv(Case):
+    def __init__(self, grids, ranks, heads, hd, bias=True, offsets=None, split=None, base=10000.0, seed=2):
+        import torch
+        lengths = [a * b * c for a, b, c in grids]
+        super().__init__(lengths, ranks, heads * hd, 3 * heads * hd, 3, bias, seed)
+        self.grids, self.heads, self.hd, self.base = grids, heads, hd, base
+        hw = 2 * (hd // 6)
+        self.split = split or (hd - 2 * hw, hw, hw)
+        self.offsets = offsets or [(i, 3 * i, 2) for i in range(len(grids))]
+        gen = torch.Generator(device="cuda").manual_seed(77 + seed)
+        self.gains = [1.0 + 0.2 * torch.randn(heads, hd, generator=gen, device="cuda") for _ in range(2)]
+
+    def run(self):
+        import torch
+        out = [torch.full((self.n + 2, self.heads, self.hd), 77.0, dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+        ropes = [lp.make_rope(g if g[0] * g[1] * g[2] else (1, 1, 1), o, self.split, self.base, self.hd) for g, o in zip(self.grids, self.offsets)]
+        ws, size = self.workspace() if max(self.ranks) else (None, 0)
+        lp.lp_qkv_projection_adapters(self.x, self.w, self.bias, self.gains[0], self.gains[1], EPS, ropes, *out, lp.make_requests(self.starts),
+                                      self.heads, self.hd, lp.make_adapters(self.adapters), ws, size, torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        assert all((t[self.n:] == 77.0).all() for t in out)
+        return [t[:self.n] for t in out]
+
+    def angles(self):
+        import torch
+        out = []
+        for g, o in zip(self.grids, self.offsets):
+            i = torch.arange(g[0] * g[1] * g[2], device="cuda")
+            where = (i // (g[1] * g[2]) + o[0], i // g[2] % g[1] + o[1], i % g[2] + o[2]) if len(i) else (i, i, i)
+            out.append(torch.stack([where[ax].double() * self.base ** (-2.0 * j / p) for ax, p in enumerate(self.split) for j in range(p // 2)], 1))
+        return torch.cat(out)
+
+    def check(self, rows=slice(None)):
+        import torch
+        got = self.run()
+        y, off = self.want(rows)
+        m, dm = y.shape[0], self.heads * self.hd
+        inside(got[2][rows].reshape(m, dm), y[:, 2 * dm:], off[:, 2 * dm:], "v")
+        angle = self.angles()[rows][:, None]
+        cos, sin = angle.cos(), angle.sin()
+        turn = (angle.abs() + 1.0) * 2.0 ** -21 + 2.0 ** -18
+        for p, name in enumerate("qk"):
+            z = y[:, p * dm:(p + 1) * dm].reshape(m, self.heads, self.hd)
+            o = off[:, p * dm:(p + 1) * dm].reshape(m, self.heads, self.hd)
+            inv = 1.0 / torch.sqrt((z * z).mean(-1, keepdim=True) + EPS)
+            gain = self.gains[p].double()
+            v = z * inv * gain
+            ov = inv * gain.abs() * (o + (z * inv).abs() * o.max(-1, keepdim=True).values) + 2.0 ** -20 * v.abs()
+            a, b, oa, ob = v[..., 0::2], v[..., 1::2], ov[..., 0::2], ov[..., 1::2]
+            size = oa + ob + turn * (a.abs() + b.abs())
+            want = torch.stack((a * cos - b * sin, a * sin + b * cos), -1).reshape(m, dm)
+            inside(got[p][rows].reshape(m, dm), want, torch.stack((size, size), -1).reshape(m, dm), name)
+        assert all(torch.isfinite(t.float()).all() for t in got)
+
+
+@pytest.mark.parametrize("grids,ranks,heads,hd", [
+    ([(1, 1, 1)], [8], 2, 64), ([(1, 1, 1)] * 3 + [(2, 1, 1)], [8, 0, 16, 8], 1, 128),
+    ([(2, 5, 7), (1, 1, 1), (3, 3, 4)], [16, 0, 40], 2, 64), ([(3, 4, 30), (5, 2, 9)], [32, 256], 1, 128),
+    ([(3, 10, 13), (3, 10, 13), (0, 1, 1), (7, 3, 11)], [64, 64, 8, 16], 12, 128),
+    ([(1, 1, 3)] * 64, [8 * (i % 3) for i in range(64)], 4, 64), ([(5, 7, 3), (2, 2, 2)], [0, 0], 4, 64),
+])
+def test_qkv_adapters(grids, ranks, heads, hd):
+    Qkv(grids, ranks, heads, hd).check()
+    Qkv(grids, ranks, heads, hd, bias=False, split=(hd, 0, 0), base=100.0).check()
+
+
+@pytest.mark.parametrize("heads,hd,grid,tiles", [
+    (2, 64, (3, 23, 39), "128x64"), (8, 128, (3, 5, 9), "128x64"), (1, 128, (1, 5, 5), "128x64"), (16, 64, (3, 13, 17), "128x128"),
+    (8, 128, (3, 20, 20), "128x128"), (36, 128, (6, 10, 10), "128x128+128x64"), (8, 64, (23, 13, 9), "256x128"), (4, 128, (9, 23, 13), "256x128"),
+    (8, 64, (11, 33, 15), "256x256"), (10, 128, (7, 23, 23), "256x256"), (6, 64, (22, 18, 33), "256x256+128x64"),
+    (12, 128, (9, 20, 20), "256x256+128x64"), (10, 64, (18, 27, 19), "256x256+128x128"), (6, 128, (19, 12, 36), "256x256+128x128"),
+    (10, 64, (18, 19, 30), "256x256+256x128"), (3, 128, (16, 34, 33), "256x256+256x128"),
+])
+def test_qkv_adapters_of_every_tiling(heads, hd, grid, tiles):
+    """The grid in three requests along its first axis, as far as it has them."""
+    import torch
+    t = grid[0]
+    grids = [(a,) + grid[1:] for a in (t - t // 2 - t // 3, t // 3, t // 2)]
+    c = Qkv(grids, [32, 0, 16], heads, hd)
+    assert str(way(c.lengths, c.ranks, c.d_in, c.d_out, hd)) == tiles
+    edges = [s + i for s in c.starts for i in (-2, -1, 0, 1) if 0 <= s + i < c.n]
+    c.check(torch.tensor(sorted(set(edges + list(range(0, c.n, max(1, c.n // 150))))), device="cuda"))
+
+
+def test_qkv_without_adapters_is_the_plain_projection_of_each_request():
+    import torch
+    c = Qkv([(3, 5, 7), (2, 9, 4)], [0, 0], 4, 128)
+    got = c.run()
+    for r, (g, o) in enumerate(zip(c.grids, c.offsets)):
+        rows = slice(c.starts[r], c.starts[r + 1])
+        plain = [torch.empty(c.lengths[r], c.heads, c.hd, dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+        lp.lp_qkv_projection(c.x[rows], c.w, c.bias, c.gains[0], c.gains[1], EPS, lp.make_rope(g, o, head_dim=c.hd), *plain, c.lengths[r], c.heads, c.hd,
+                             torch.cuda.current_stream().cuda_stream)
+        for a, b in zip(got, plain):
+            # another tiling may add up in another order; the rounding is the same but where a sum lies next to a border
+            assert (a[rows].float() - b.float()).abs().max() <= 2.0 ** -7 * b.float().abs().max()
+
+
+# ---- as they are used
+
+def test_two_calls_on_two_streams_with_a_workspace_each():
+    import torch
+    a, b = Case([900, 600], [64, 16], 1536, 1536, seed=3), Case([700, 800], [32, 32], 1536, 1536, seed=4)
+    want = [c.linear().clone() for c in (a, b)]
+    streams, outs = [torch.cuda.Stream(), torch.cuda.Stream()], []
+    for c in (a, b):
+        outs.append((torch.empty(c.n, c.d_out, dtype=torch.bfloat16, device="cuda"), c.workspace()))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for c, st, (y, (ws, size)) in zip((a, b), streams, outs):
+            lp.lp_linear_adapters(c.x, c.w, c.bias, y, lp.make_requests(c.starts), c.d_in, c.d_out, lp.make_adapters(c.adapters), ws, size, st.cuda_stream)
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, w) for (y, _), w in zip(outs, want))
+
+
+def test_the_blocks_of_two_requests_from_a_graph():
+    """The self-attention half of a block over a packed batch: modulated norm, projection with adapters, attention per request, output projection with
+    adapters, gated residual and the next norm.  Replayed with other inputs, and every link against its definition on what it was given."""
+    import torch
+    from tests import gpu_util as g
+    heads, hd, grids, ranks = 4, 64, [(3, 8, 9), (2, 11, 10)], [16, 32]
+    dm = heads * hd
+    q = Qkv(grids, ranks, heads, hd, seed=11)
+    o = Case(q.lengths, ranks[::-1], dm, dm, seed=12)
+    n, starts = q.n, q.starts
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    f = lambda *shape: torch.randn(shape, generator=gen, device="cuda")
+    h, mod = f(n, dm), 0.3 * f(2, 6, dm)
+    h_out, normed, y, last = torch.empty_like(h), torch.empty(n, dm, dtype=torch.bfloat16, device="cuda"), *(
+        torch.empty(n, dm, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    qkv = [torch.empty(n, heads, hd, dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+    att = torch.empty_like(qkv[0])
+    req, norm = lp.make_requests(starts), lp.make_norm(lp.LP_NORM_LAYER, EPS)
+    m1, m2 = lp.make_modulation(scale=mod[:, 0], shift=mod[:, 1]), lp.make_modulation(gate=mod[:, 2], scale=mod[:, 3], shift=mod[:, 4])
+    ropes = [lp.make_rope(gr, off, q.split, q.base, hd) for gr, off in zip(grids, q.offsets)]
+    tq, to = lp.make_adapters(q.adapters), lp.make_adapters(o.adapters)
+    (ws, size), (aws, asize) = q.workspace(), g.workspace(hd)
+
+    def half():
+        st = torch.cuda.current_stream().cuda_stream
+        lp.lp_norm_modulate(h, lp.LP_F32, normed, req, dm, norm, m1, stream=st)
+        lp.lp_qkv_projection_adapters(normed, q.w, q.bias, q.gains[0], q.gains[1], EPS, ropes, *qkv, req, heads, hd, tq, ws, size, st)
+        for a, b in zip(starts, starts[1:]):
+            lp.lp_attention(*(t[a:b] for t in qkv), att[a:b], b - a, heads, hd, dm, hd, 0.0, aws, asize, st)
+        lp.lp_linear_adapters(att, o.w, o.bias, y, req, dm, dm, to, ws, size, st)
+        lp.lp_gated_residual_norm(h, lp.LP_F32, y, h_out, last, req, dm, None, norm, m2, stream=st)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        half()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        half()
+    results = (normed, *qkv, att, y, h_out, last)
+    for scale in (1.0, 0.3, 4.0):
+        h.mul_(scale)
+        for t in results:
+            t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in results]
+        half()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, results))
+    # every link on its own inputs: rounding to bf16 and 2^-12 of the terms, which the finer tests above hold it to
+    spread = lambda v: torch.repeat_interleave(v.double(), torch.tensor(q.lengths, device="cuda"), 0)
+    layer = lambda t: (t - t.mean(-1, keepdim=True)) / torch.sqrt(t.var(-1, unbiased=False, keepdim=True) + EPS)
+    close = lambda a, want, slack: inside(a, want, torch.full_like(want, slack))
+    close(normed, layer(h.double()) * (1 + spread(mod[:, 0])) + spread(mod[:, 1]), 2.0 ** -12)
+    q.x = normed
+    yq, off = q.want()
+    inside(qkv[2].reshape(n, dm), yq[:, 2 * dm:], off[:, 2 * dm:])
+    for a, b in zip(starts, starts[1:]):
+        qq, kk, vv = (t[a:b].float().permute(1, 0, 2).double() for t in qkv)
+        p = torch.softmax(torch.matmul(qq, kk.transpose(1, 2).contiguous()) / hd ** 0.5, -1)
+        err = (att[a:b].double() - torch.matmul(p, vv.contiguous()).permute(1, 0, 2)).abs()
+        assert float(err.max()) <= 2e-2 * float(vv.abs().max()) and float(err.mean()) <= 2e-3 * float(vv.abs().max())
+    o.x = att.reshape(n, dm)
+    inside(y, *o.want())
+    hw = h.double() + spread(mod[:, 2]) * y.double()
+    close(h_out, hw, 2.0 ** -12 * float(hw.abs().max()))
+    close(last, layer(hw) * (1 + spread(mod[:, 3])) + spread(mod[:, 4]), 2.0 ** -12)

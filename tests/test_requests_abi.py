@@ -69,3 +69,77 @@ def test_modulation_of_tensors_takes_their_stride():
     assert lp.make_modulation(scale=t[0, 0]).stride == 0 and lp.make_modulation().stride == 0
     with pytest.raises(ValueError):
         lp.make_modulation(scale=t[:, 0], shift=t[0, 1])
+
+
+def _adapters(*specs):
+    """(down, up, rank, scale) as given, addresses unchecked."""
+    return (lp.lp_adapter * max(len(specs), 1))(*[lp.lp_adapter(*s) for s in specs])
+
+
+GOOD = (1 << 24, 1 << 25, 16, 1.0)
+
+
+def _linear(x=1 << 20, w=1 << 21, bias=None, y=1 << 22, starts=(0, 3), d_in=128, d_out=256, adapters=None, ws=1 << 26, size=1 << 20):
+    adapters = _adapters(GOOD) if adapters is None else adapters
+    return lp._lib().lp_linear_adapters(x, w, bias, y, lp._ref(lp.make_requests(starts)), d_in, d_out, None if adapters == "null" else adapters, ws, size, None)
+
+
+def test_linear_adapters_refusals():
+    inv, uns = lp.LP_ERR_INVALID_ARG, lp.LP_ERR_UNSUPPORTED
+    for name in ("x", "w", "y"):
+        assert _linear(**{name: None}) == inv and _linear(**{name: (1 << 22) + 8}) == inv
+    assert _linear(bias=4) == inv and _linear(y=1 << 20) == inv and _linear(y=1 << 21) == inv
+    assert _linear(d_in=100) == uns and _linear(d_out=192) == uns and _linear(d_in=0) == inv
+    assert _linear(adapters="null") == inv and _linear(starts=(0, 3, 2)) == inv and _linear(starts=range(66)) == lp.LP_ERR_LIMIT
+    for bad, status in (((1 << 24, 1 << 25, -8, 1.0), inv), ((1 << 24, 1 << 25, 4, 1.0), uns), ((1 << 24, 1 << 25, 264, 1.0), uns),
+                        ((None, 1 << 25, 8, 1.0), inv), ((1 << 24, None, 8, 1.0), inv), (((1 << 24) + 8, 1 << 25, 8, 1.0), inv),
+                        ((1 << 24, (1 << 25) + 2, 8, 1.0), inv), ((1 << 24, 1 << 25, 8, NAN), inv), ((1 << 24, 1 << 25, 8, INF), inv)):
+        assert _linear(adapters=_adapters(bad)) == status
+        assert _linear(starts=(0, 3, 3), adapters=_adapters(GOOD, bad)) == status               # of a request without rows too
+    assert _linear(ws=None) == inv and _linear(ws=(1 << 26) + 8) == inv and _linear(size=4224 + 3 * 128 - 1) == inv
+    assert _linear(ws=1 << 20) == inv and _linear(ws=1 << 21) == inv and _linear(ws=1 << 22) == inv
+    # nothing to do
+    assert _linear(None, None, None, None, (0, 0), ws=None, size=0) == lp.LP_OK and _linear(starts=(), adapters="null") == lp.LP_OK
+
+
+def test_workspace_size():
+    size = lp._lib().lp_adapter_workspace_size
+    assert size(10, 8, 1) == size(10, 32, 1) == 4224 + 10 * 128 and size(10, 33, 1) == 4224 + 10 * 256
+    assert size(10, 256, 3) == 4224 + 10 * 3 * 8 * 128
+    assert size(0, 8, 1) == 0 and size(10, 0, 3) == 0
+    assert size(-1, 8, 1) == size(1, -8, 1) == size(1, 8, 2) == lp.LP_ERR_INVALID_ARG
+    assert size(1, 264, 1) == size(2 ** 31 - 1, 8, 1) == lp.LP_ERR_UNSUPPORTED
+    with pytest.raises(lp.LPError):
+        lp.lp_adapter_workspace_size(1, 8, 2)
+
+
+def _qkv(x=1 << 20, w=1 << 21, gq=1 << 22, gk=1 << 23, q=1 << 27, k=1 << 28, v=1 << 29, eps=1e-6, starts=(0, 4, 4, 10), heads=2, hd=64, ropes=None,
+         adapters=None, ws=1 << 26, size=1 << 20):
+    if ropes is None:
+        ropes = [lp.make_rope((1, 2, 2), head_dim=64), lp.make_rope((9, 9, 9), split=(0, 0, 64), base=5.0, head_dim=64), lp.make_rope((1, 1, 6), head_dim=64)]
+    ropes = (lp.lp_rope * 3)(*ropes) if ropes != "null" else None
+    return lp._lib().lp_qkv_projection_adapters(x, w, None, gq, gk, eps, ropes, q, k, v, lp._ref(lp.make_requests(starts)), heads, hd,
+                                                _adapters(GOOD, GOOD, GOOD) if adapters is None else adapters, ws, size, None)
+
+
+def test_qkv_adapters_refusals():
+    inv, uns = lp.LP_ERR_INVALID_ARG, lp.LP_ERR_UNSUPPORTED
+    for name in ("x", "w", "gq", "gk", "q", "k", "v"):
+        assert _qkv(**{name: None}) == inv and _qkv(**{name: (1 << 22) + 8}) == inv
+    assert _qkv(ropes="null") == inv and _qkv(heads=0) == inv and _qkv(hd=96) == uns and _qkv(heads=3) == uns and _qkv(eps=-1.0) == inv
+    rope = lambda *a, **kw: lp.make_rope(*a, head_dim=64, **kw)
+    fine = [rope((1, 2, 2)), rope((9, 9, 9)), rope((1, 1, 6))]
+    for i, bad in ((0, rope((1, 2, 3))), (2, rope((6, 1, 1), base=5.0)), (2, rope((6, 1, 1), split=(20, 24, 20))), (2, rope((6, 1, 1), split=(23, 21, 20))),
+                   (0, rope((-2, -2, 1))), (0, rope((1, 2, 2), base=-1.0))):
+        assert _qkv(ropes=fine[:i] + [bad] + fine[i + 1:]) == inv
+    assert _qkv(q=1 << 28) == inv and _qkv(v=1 << 20) == inv
+    assert _qkv(ws=None) == inv and _qkv(size=4224 + 10 * 3 * 128 - 1) == inv and _qkv(ws=1 << 27) == inv
+    assert _qkv(starts=(0, 0, 0, 0)) == lp.LP_OK
+
+
+def test_tables_shorter_than_the_requests_are_refused():
+    req = lp.make_requests([0, 2, 4, 6])
+    with pytest.raises(ValueError):
+        lp.lp_linear_adapters(1 << 20, 1 << 21, None, 1 << 22, req, 64, 128, lp.make_adapters([None]))
+    with pytest.raises(ValueError):
+        lp.lp_qkv_projection_adapters(1, 2, None, 3, 4, 1e-6, [lp.make_rope((1, 1, 2))], 5, 6, 7, req, 1, 128, lp.make_adapters([None] * 3))
