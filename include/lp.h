@@ -358,7 +358,7 @@ int lp_qkv_projection_adapters(const void *x, const void *w_qkv, const float *bi
                                void *workspace, int64_t workspace_bytes, void *stream);
 
 /* Bytes of workspace for n_tokens rows and adapters of up to `rank`; sections: 1 (lp_linear_adapters) or 3
- * (lp_qkv_projection_adapters).  128 bytes per row, section and 32 ranks, and 4224.  Negative LP_ERR_* on failure. */
+ * (lp_qkv_projection_adapters).  128 bytes per row, section and 32 ranks, and 3200.  Negative LP_ERR_* on failure. */
 int64_t lp_adapter_workspace_size(int64_t n_tokens, int32_t rank, int32_t sections);
 
 #define LP_BF16 0 /* element types of the residual stream */

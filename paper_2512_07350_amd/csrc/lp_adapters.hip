@@ -17,7 +17,7 @@ namespace {
 // ---- the down products
 
 struct DownRun {
-    int32_t start, rank;                 // as AdapterRun
+    int32_t start, rank;                 // rows from start on, to the next run's; rank 0: no adapter
     int32_t first, first_look;           // the run's first workgroup, that of those that look over U
     float scale;
     const __bf16 *down, *up;             // D [sections * rank, d_in], U [d_out, rank]
@@ -25,25 +25,25 @@ struct DownRun {
 struct DownArgs {
     const __bf16 *x;
     __bf16 *t;                           // see AdaptedArgs
-    uint32_t *control;
+    AdapterControl *control;
     int32_t t_row, t_blocks, d_in, d_out, sections, looks;
     DownRun run[LP_MAX_REQUESTS + 1];
 };
 
-// 16 bytes of U to a workgroup's look, in pieces of which a run has at most kLooks.
-__host__ __device__ int32_t look_pieces(int64_t pieces) {
+// Workgroups that look over a U of `pieces` 16 bytes: one for 64 KB, at most kLooks.
+__host__ __device__ int32_t look_parts(int64_t pieces) {
     const int64_t by_size = (pieces + 4095) / 4096;
     return int32_t(by_size < kLooks ? by_size : kLooks);
 }
 
 using DownTile = Tiling<2, 2, 2, 1, 8, kSplitK>;         // 64 rows of D x 32 tokens, four wavefronts sharing k
 
-// Whether part of a run's U holds an infinity or a NaN, to its word of the control block; 64 KB to a workgroup up to 1 MB.
+// Whether part of a run's U holds an infinity or a NaN, to its word of the control block; the first workgroup writes the rest of the block.
 __device__ void look_over(const DownArgs &a, int wg) {
     const int r = __builtin_amdgcn_readfirstlane(__popcll(__ballot(a.run[threadIdx.x % 64].first_look <= wg))) - 1;
     const int part = wg - a.run[r].first_look;
     const int64_t pieces = int64_t(a.d_out) * a.run[r].rank / 8;
-    const int parts = look_pieces(pieces);
+    const int parts = look_parts(pieces);
     const uint4 *u = reinterpret_cast<const uint4 *>(a.run[r].up);
     const int64_t last = pieces * (part + 1) / parts;
     uint32_t bad = 0;
@@ -57,10 +57,15 @@ __device__ void look_over(const DownArgs &a, int wg) {
         look(p.w);
     }
     const int any = __syncthreads_or(int(bad));
-    uint32_t *words = a.control + kControlNan + r * kLooks;
-    if (threadIdx.x == 0) words[part] = uint32_t(any);
-    if (part == 0 && int(threadIdx.x) >= parts && threadIdx.x < kLooks) words[threadIdx.x] = 0;
-    if (wg == 0 && threadIdx.x < kControlNan) a.control[threadIdx.x] = 0x7fc07fc0u;
+    const int i = int(threadIdx.x);
+    if (i == 0) a.control->looks[r][part] = uint32_t(any);
+    if (part == 0 && i >= parts && i < kLooks) a.control->looks[r][i] = 0;
+    if (wg == 0 && i < LP_MAX_REQUESTS) {
+        a.control->run[i] = AdapterRun{a.run[i].start, a.run[i + 1].start, a.run[i].rank, 0, a.run[i].up, 0};
+        if (i < 32) a.control->nan[i] = 0x7fc07fc0u;
+        if (a.run[i].rank == 0)
+            for (int k = 0; k < kLooks; ++k) a.control->looks[i][k] = 0;
+    }
 }
 
 __global__ __launch_bounds__(DownTile::kThreads, 1) void adapter_down_kernel(const DownArgs a) {
@@ -81,7 +86,7 @@ __global__ __launch_bounds__(DownTile::kThreads, 1) void adapter_down_kernel(con
     g.d_in = a.d_in;
     g.d_out = rows;
     f32x4 acc[C::FB][C::TB];
-    product_split_k<C>(lds0, g, f0, t0, wave, lane, acc);
+    product_split_k<C>(lds0, g, f0, t0, wave, lane, acc, 0);
     const float scale = a.run[r].scale;
     const int tok = t0 + wave % C::WT * 16 + col;
 #pragma unroll
@@ -107,7 +112,6 @@ struct Runs {
     int32_t runs = 0, largest = 0;       // runs; the largest rank
     int64_t workgroups = 0;              // of the down products
     DownArgs down{};
-    AdapterRun run[LP_MAX_REQUESTS + 1];
 };
 
 int make_runs(const lp_requests *requests, const lp_adapter *adapters, int32_t d_in, int32_t d_out, int32_t sections, Runs *out) {
@@ -131,22 +135,19 @@ int make_runs(const lp_requests *requests, const lp_adapter *adapters, int32_t d
         last = &ad;
         if (same) continue;
         const int i = out->runs++;
-        out->run[i] = AdapterRun{q.start[r], ad.rank, static_cast<const __bf16 *>(ad.up)};
         out->down.run[i] = DownRun{q.start[r], ad.rank, 0, 0, ad.scale, static_cast<const __bf16 *>(ad.down), static_cast<const __bf16 *>(ad.up)};
         if (ad.rank > out->largest) out->largest = ad.rank;
     }
     const int32_t n = int32_t(q.rows());
-    for (int i = out->runs; i <= LP_MAX_REQUESTS; ++i) {
-        out->run[i] = AdapterRun{i == out->runs ? n : INT32_MAX, 0, nullptr};
+    for (int i = out->runs; i <= LP_MAX_REQUESTS; ++i)
         out->down.run[i] = DownRun{i == out->runs ? n : INT32_MAX, 0, INT32_MAX, INT32_MAX, 0.0f, nullptr, nullptr};
-    }
     for (int i = 0; i < out->runs; ++i) {
-        const int64_t tokens = (int64_t(out->run[i + 1].start) - out->run[i].start + DownTile::kT - 1) / DownTile::kT;
-        const int64_t rows = (int64_t(sections) * out->run[i].rank + DownTile::kF - 1) / DownTile::kF;
+        const int64_t tokens = (int64_t(out->down.run[i + 1].start) - out->down.run[i].start + DownTile::kT - 1) / DownTile::kT;
+        const int64_t rows = (int64_t(sections) * out->down.run[i].rank + DownTile::kF - 1) / DownTile::kF;
         out->down.run[i].first = int32_t(out->workgroups);
         out->workgroups += tokens * rows;
         out->down.run[i].first_look = out->down.looks;
-        out->down.looks += look_pieces(int64_t(d_out) * out->run[i].rank / 8);
+        out->down.looks += look_parts(int64_t(d_out) * out->down.run[i].rank / 8);
         if ((out->workgroups + out->down.looks) * DownTile::kThreads > lp::kMaxLaunchThreads) return LP_ERR_UNSUPPORTED;
     }
     out->down.d_in = d_in;
@@ -156,8 +157,8 @@ int make_runs(const lp_requests *requests, const lp_adapter *adapters, int32_t d
 }
 
 // The tiling of a call: pick_plan's, with the k-tiles of the adapters that a tile of t tokens takes on average.
-Plan pick_adapted(int32_t n, int32_t d_in, int32_t d_out, int32_t head_dim, int cus, int32_t runs, const AdapterRun *run) {
-    return pick_plan(n, d_out, false, cus, [&](int t) {
+Plan pick_adapted(int32_t n, int32_t d_in, int32_t d_out, int32_t head_dim, int cus, int32_t runs, const DownRun *run) {
+    return pick_plan(n, d_out, small_tilings(head_dim), cus, [&](int t) {
         int64_t extra = 0;
         for (int i = 0; i < runs; ++i) {
             const int64_t first = run[i].start / t, last = (run[i + 1].start - 1) / t;
@@ -176,10 +177,10 @@ int project(AdaptedArgs<QKV> &a, Runs &runs, void *workspace, int64_t workspace_
     int dev = 0;
     const int cus = lp::device_compute_units(&dev);
     if (cus <= 0) return LP_ERR_HIP;
+    DownArgs &d = runs.down;
     if (runs.largest > 0) {
-        DownArgs &d = runs.down;
         d.x = a.x;
-        d.control = static_cast<uint32_t *>(workspace);
+        d.control = static_cast<AdapterControl *>(workspace);
         d.t = static_cast<__bf16 *>(workspace) + kControlBytes / 2;
         d.t_row = int32_t(t_row);
         d.t_blocks = (runs.largest + kRanks - 1) / kRanks;
@@ -194,19 +195,7 @@ int project(AdaptedArgs<QKV> &a, Runs &runs, void *workspace, int64_t workspace_
         a.t_row = d.t_row;
         a.t_blocks = d.t_blocks;
     }
-    a.runs = runs.runs;
-    for (int i = 0; i <= LP_MAX_REQUESTS; ++i) a.run[i] = runs.run[i];
-    const Plan p = pick_adapted(a.n, a.d_in, a.d_out, QKV ? HD : 0, cus, runs.runs, runs.run);
-    switch (p.tile * 8 + p.cut + 1) {
-        case 0 * 8 + 2: return launch_tiles<QKV, HD, Tile256x256, Tile256x128>(a, p.whole, stream);
-        case 0 * 8 + 3: return launch_tiles<QKV, HD, Tile256x256, Tile128x128>(a, p.whole, stream);
-        case 0 * 8 + 4: return launch_tiles<QKV, HD, Tile256x256, Tile128x64>(a, p.whole, stream);
-        case 2 * 8 + 4: return launch_tiles<QKV, HD, Tile128x128, Tile128x64>(a, p.whole, stream);
-        case 1 * 8: return launch_tiles<QKV, HD, Tile256x128, Tile256x128>(a, p.whole, stream);
-        case 2 * 8: return launch_tiles<QKV, HD, Tile128x128, Tile128x128>(a, p.whole, stream);
-        case 3 * 8: return launch_tiles<QKV, HD, Tile128x64, Tile128x64>(a, p.whole, stream);
-        default: return launch_tiles<QKV, HD, Tile256x256, Tile256x256>(a, p.whole, stream);
-    }
+    return launch_plan<QKV, HD>(pick_adapted(a.n, a.d_in, a.d_out, QKV ? HD : 0, cus, runs.runs, d.run), a, stream);
 }
 
 }  // namespace
@@ -214,14 +203,14 @@ int project(AdaptedArgs<QKV> &a, Runs &runs, void *workspace, int64_t workspace_
 // For the tests, as lp_internal_gemm_way: rows and ranks of the requests.
 extern "C" int lp_internal_adapted_way(const int64_t *start, const int32_t *rank, int32_t count, int32_t d_in, int32_t d_out, int32_t head_dim,
                                        int32_t cus, int64_t way[6]) {
-    AdapterRun run[LP_MAX_REQUESTS + 1];
+    DownRun run[LP_MAX_REQUESTS + 1];
     int runs = 0;
     for (int r = 0; r < count; ++r)
-        if (start[r + 1] > start[r]) run[runs++] = AdapterRun{int32_t(start[r]), rank[r], nullptr};
-    run[runs] = AdapterRun{int32_t(start[count]), 0, nullptr};
+        if (start[r + 1] > start[r]) run[runs++] = DownRun{int32_t(start[r]), rank[r], 0, 0, 0.0f, nullptr, nullptr};
+    run[runs] = DownRun{int32_t(start[count]), 0, 0, 0, 0.0f, nullptr, nullptr};
     const int64_t n = start[count];
     const Plan p = pick_adapted(int32_t(n), d_in, d_out, head_dim, cus, runs, run);
-    plan_way(p, n, d_out, false, way);
+    plan_way(p, n, d_out, head_dim == 0 && four_waves(p, d_in), way);
     return LP_OK;
 }
 

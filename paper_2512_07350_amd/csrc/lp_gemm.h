@@ -62,20 +62,28 @@ struct GemmArgs {
 // A row of another request meets U_r with zeros for t.  An infinity or a NaN in U_r would reach it all the same (0 x inf), so that
 // adapter_down_kernel has looked over every U_r: one that holds any is taken as zeros, and the t of its own rows as NaN.
 constexpr int kRanks = 32;               // ranks of a k-tile
-constexpr int kLooks = 16;               // words of a run that say whether parts of its U are not finite
-constexpr int kControlNan = 32;          // the control block in front of t: a k-tile's row of NaN, then kLooks words a run
-constexpr int kControlBytes = 4 * (kControlNan + LP_MAX_REQUESTS * kLooks);
+constexpr int kLooks = 4;                // words of a run that say whether parts of its U are not finite
 struct AdapterRun {
-    int32_t start, rank;                 // rows from start on, to the next run's; rank 0: no adapter
+    int32_t start, end, rank;            // rows; rank 0: no adapter
+    int32_t unused;
     const __bf16 *up;                    // U [d_out, rank]
+    uint64_t unused8;
 };
+// In front of t in the workspace, written by adapter_down_kernel.  A tile has the tables in LDS (kTableBytes behind its stages), loaded in front of its
+// first k-tiles and read behind its last, so that it waits for them nowhere.
+struct AdapterControl {
+    uint32_t nan[32];                    // a k-tile's row of t that is NaN throughout
+    uint32_t looks[LP_MAX_REQUESTS][kLooks];
+    AdapterRun run[LP_MAX_REQUESTS];
+};
+constexpr int kControlBytes = sizeof(AdapterControl), kTableBytes = kControlBytes - sizeof(AdapterControl::nan);
+static_assert(kTableBytes == 3 * 1024 && sizeof(AdapterRun) == 32, "whole loads");
 template <bool QKV>
 struct AdaptedArgs : GemmArgs {
     // t: row i at i * t_row bytes, per section (q, k, v; one otherwise) t_blocks groups of 32 ranks: 32 values, then what they leave
     const __bf16 *t;
-    const uint32_t *control;
-    int32_t t_row, t_blocks, runs;
-    AdapterRun run[LP_MAX_REQUESTS + 1];         // entries past the last start behind every row
+    const AdapterControl *control;       // nullptr: no run has an adapter
+    int32_t t_row, t_blocks;
 };
 // QKV: where the tokens of each request are rotated to.
 struct RequestGrid {
@@ -139,45 +147,57 @@ struct Tiling {
 };
 
 // The k-tiles of the adapters of one tile: kF features from f0 on, kT tokens from t0 on.  Everything is the same in all lanes
-// (scalar registers) but the offsets of a load.
+// (scalar registers) but the runs, one to a lane, and the offsets of a load.
 template <typename C, typename Args>
 struct AdapterTiles {
     static constexpr bool QKV = std::is_same<Args, AdaptedArgs<true>>::value;
     const Args &a;
     const int f0, t0;
-    uint64_t left = 0;                   // runs still to come, the present one included
-    int count = 0;                       // k-tiles in all
-    int first_section, last_section;
-    // the present one
-    int section = 0, block = 0, blocks = 0;
+    const uint32_t table;                // LDS
+    uint64_t left = 0, not_finite = 0;   // runs still to come, the present one included; those whose U is not finite
+    int first_section, last_section, section;
+    int block = 0, blocks = 0;           // of the present run
     uint32_t granules = 0, t_col = 0;    // 16-byte pieces of U's rows; offset of the k-tile in t's
     uint32_t t_row = 0;                  // bytes from row to row of t; 0: every row is the one of NaN, U is zeros
     int t_lo = 0, t_hi = 0, f_lo = 0, f_hi = 0;          // rows of the tile that are the run's, features that are the section's
+    int32_t start, end, rank;            // of run `lane`
+    uint32_t up_lo, up_hi;
     __amdgpu_buffer_rsrc_t u_rsrc, t_rsrc;
 
-    __device__ __forceinline__ AdapterTiles(const Args &args, int f, int t, int lane) : a(args), f0(f), t0(t) {
+    __device__ __forceinline__ AdapterTiles(const Args &args, int f, int t, uint32_t table_lds) : a(args), f0(f), t0(t), table(table_lds) {
         const int dm = QKV ? a.d_out / 3 : a.d_out;
         first_section = f0 / dm;
         last_section = min(f0 + C::kF - 1, a.d_out - 1) / dm;
-        const int32_t start = a.run[lane].start, end = a.run[lane + 1].start, rank = a.run[lane].rank;
-        const int of_run = rank > 0 && start - t0 < C::kT && end > t0 ? (rank + kRanks - 1) / kRanks : 0;
-        left = __ballot(of_run > 0);
-        for (uint64_t m = left; m != 0; m &= m - 1) count += __builtin_amdgcn_readlane(of_run, __builtin_ctzll(m));
-        count *= last_section - first_section + 1;
         section = last_section;          // next() turns to the first run
-        u_rsrc = t_rsrc = buffer(a.t, 0);
+        u_rsrc = t_rsrc = buffer(nullptr, 0);
     }
     __device__ __forceinline__ static __amdgpu_buffer_rsrc_t buffer(const void *p, int64_t bytes) {
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, int(bytes), 0x00020000);
     }
-    // Scalar loads: a vector load would be waited for behind all that is on its way to LDS.
-    __device__ __forceinline__ bool not_finite(int r) const {
-        typedef __attribute__((address_space(4))) const uint32_t Words;
-        Words *w = (Words *)(uintptr_t(a.control + kControlNan + r * kLooks));
-        uint32_t any = 0;
-#pragma unroll
-        for (int i = 0; i < kLooks; ++i) any |= w[i];
-        return any != 0;
+    // Sends for the tables.
+    __device__ __forceinline__ void send(int wave, int lane) {
+        if (a.control == nullptr || wave >= kTableBytes / 1024) return;
+        load_to_lds_16(buffer(a.control->looks, kTableBytes), __builtin_amdgcn_readfirstlane(table + wave * 1024), 16 * lane,
+                       __builtin_amdgcn_readfirstlane(wave * 1024));
+    }
+    // The k-tiles in all.  The tables have landed (a barrier ago).
+    __device__ __forceinline__ int look(int lane) {
+        if (a.control == nullptr) return 0;
+        const u32x4 words = lds_load<u32x4>(table + 4 * kLooks * lane);
+        const uint32_t at = table + 4 * kLooks * LP_MAX_REQUESTS + uint32_t(sizeof(AdapterRun)) * lane;
+        const u32x4 rows = lds_load<u32x4>(at);
+        const u32x2 up = lds_load<u32x2>(at + 16);
+        start = int32_t(rows.x);
+        end = int32_t(rows.y);
+        rank = int32_t(rows.z);
+        up_lo = up.x;
+        up_hi = up.y;
+        not_finite = __ballot((words.x | words.y | words.z | words.w) != 0);
+        const int tiles = rank > 0 && start - t0 < C::kT && end > t0 ? (rank + kRanks - 1) / kRanks : 0;
+        left = __ballot(tiles > 0);
+        int count = 0;
+        for (uint64_t m = left; m != 0; m &= m - 1) count += __builtin_amdgcn_readlane(tiles, __builtin_ctzll(m));
+        return count * (last_section - first_section + 1);
     }
     // The k-tile behind the present one.  Past the last one: one of zeros.
     __device__ __forceinline__ void next() {
@@ -193,25 +213,26 @@ struct AdapterTiles {
         }
         section = section == last_section ? first_section : section + 1;
         const int r = __builtin_ctzll(left);
-        const int rank = a.run[r].rank;
-        blocks = (rank + kRanks - 1) / kRanks;
+        const int ranks = __builtin_amdgcn_readlane(rank, r);
+        blocks = (ranks + kRanks - 1) / kRanks;
         block = 0;
-        granules = uint32_t(rank) / 8;
-        t_lo = max(a.run[r].start - t0, 0);
-        t_hi = min(a.run[r + 1].start - t0, C::kT);
+        granules = uint32_t(ranks) / 8;
+        t_lo = max(__builtin_amdgcn_readlane(start, r) - t0, 0);
+        t_hi = min(__builtin_amdgcn_readlane(end, r) - t0, C::kT);
         const int dm = QKV ? a.d_out / 3 : a.d_out;
         f_lo = section * dm - f0;
         f_hi = f_lo + dm;
         const int64_t t_rows = min(int64_t(C::kT), int64_t(a.n) - t0), u_rows = min(int64_t(C::kF), int64_t(a.d_out) - f0);
-        if (not_finite(r)) {
+        if ((not_finite >> r) & 1) {
             t_row = t_col = 0;
-            t_rsrc = buffer(a.control, 4 * kRanks);
-            u_rsrc = buffer(a.run[r].up, 0);
+            t_rsrc = buffer(a.control->nan, sizeof(a.control->nan));
+            u_rsrc = buffer(nullptr, 0);
         } else {
             t_row = uint32_t(a.t_row);
             t_col = uint32_t(section) * uint32_t(a.t_blocks) * (4 * kRanks);
             t_rsrc = buffer(reinterpret_cast<const unsigned char *>(a.t) + int64_t(t0) * a.t_row, t_rows * a.t_row);
-            u_rsrc = buffer(a.run[r].up + int64_t(f0) * rank, u_rows * rank * 2);
+            const uint64_t up = uint64_t(uint32_t(__builtin_amdgcn_readlane(int(up_hi), r))) << 32 | uint32_t(__builtin_amdgcn_readlane(int(up_lo), r));
+            u_rsrc = buffer(reinterpret_cast<const unsigned char *>(up) + int64_t(f0) * ranks * 2, u_rows * ranks * 2);
         }
     }
     // Where lane `lane` of a load of rows 8 group .. 8 group + 7 fetches its granule g (0 .. 7) from; out of the buffer: zeros
@@ -228,9 +249,8 @@ struct AdapterTiles {
 };
 // What a product without adapters has instead.
 struct NoAdapterTiles {
-    static constexpr int count = 0;
     template <typename Args>
-    __device__ __forceinline__ NoAdapterTiles(const Args &, int, int, int) {}
+    __device__ __forceinline__ NoAdapterTiles(const Args &, int, int, uint32_t) {}
 };
 template <typename C, typename Args>
 using AdapterTilesOf = std::conditional_t<kAdapted<Args>, AdapterTiles<C, Args>, NoAdapterTiles>;
@@ -251,7 +271,7 @@ using AdapterTilesOf = std::conditional_t<kAdapted<Args>, AdapterTiles<C, Args>,
 // projection runs at 1050 to 1370 by the clock the card has at the time (1.98 to 1.52 ms, 1.76 on average).
 template <typename C, typename Args>
 __device__ __forceinline__ void product(uint32_t lds0, const Args &a, int f0, int t0, int wave, int lane,
-                                        f32x4 (&acc)[C::FB][C::TB]) {
+                                        f32x4 (&acc)[C::FB][C::TB], uint32_t table) {
     constexpr int FB = C::FB, TB = C::TB, FH = C::FH, S = C::S, W = C::kWaves;
     const int col = lane % 16, quad = lane / 16;
     const int fw = wave / C::WT, tw = wave % C::WT;
@@ -279,7 +299,7 @@ __device__ __forceinline__ void product(uint32_t lds0, const Args &a, int f0, in
     };
     auto load_y = [&](int i, int kt, uint32_t stage) { load(w_rsrc, lo_group(i) + kHalfGroups, kt, stage); };
     // the same for the present k-tile of the adapters
-    AdapterTilesOf<C, Args> extra(a, f0, t0, lane);
+    AdapterTilesOf<C, Args> extra(a, f0, t0, table);
     const uint32_t granule = (lane % 8) ^ swz((wave & 1) * 8 + lane / 8);
     auto load_u = [&](int group, uint32_t stage) {
         if constexpr (kAdapted<Args>)
@@ -306,7 +326,15 @@ __device__ __forceinline__ void product(uint32_t lds0, const Args &a, int f0, in
     auto read_hi = [&](int m, int s) { hi[m][s] = lds_load<bf16x8>(w_addr[s] + (FH + m) * 16 * kRowBytes); };
     auto read_x = [&](int t, int s) { xop[t][s] = lds_load<bf16x8>(x_addr[s] + t * 16 * kRowBytes); };
 
-    const int n_plain = a.d_in / kBK, n_kt = n_plain + extra.count;
+    const int n_plain = a.d_in / kBK;
+    int n_kt = n_plain;
+    if constexpr (kAdapted<Args>) {
+        extra.send(wave, lane);
+        if (n_plain < S) {                               // the adapters' k-tiles are among the first ones sent for
+            stage_barrier<0>();
+            n_kt += extra.look(lane);
+        }
+    }
 #pragma unroll
     for (int p = 0; p < S; ++p) {
         if (p < n_plain) {
@@ -411,11 +439,13 @@ __device__ __forceinline__ void product(uint32_t lds0, const Args &a, int f0, in
     };
     int kt = 0;
     for (; kt + S < n_plain; ++kt) tile(kt, std::integral_constant<int, S>{}, std::false_type{});
-    if constexpr (kAdapted<Args>)
+    if constexpr (kAdapted<Args>) {
+        if (n_plain >= S) n_kt += extra.look(lane);
         for (; kt + S < n_kt; ++kt) {
             extra.next();
             tile(kt, std::integral_constant<int, S>{}, std::true_type{});
         }
+    }
     static_for<0, S>([&](auto lc) {
         constexpr int LEFT = S - 1 - decltype(lc)::value;
         if (kt + LEFT == n_kt - 1) tile(kt++, std::integral_constant<int, LEFT>{}, std::false_type{});
@@ -452,9 +482,9 @@ __device__ __forceinline__ void load_at_m0(const __amdgpu_buffer_rsrc_t &rsrc, u
 // Not with the QKV epilogue, which one wavefront to a SIMD takes longer for, by what the products gain: 8192 x 2048 -> 6144 158.9 /
 // 170.8, 8192 x 3072 -> 9216 355 / 369, and with 80 k-tiles 8192 x 5120 -> 15360 911.5 / 910.3, 13230 x 5120 1467 / 1438,
 // 11340 x 5120 1273 / 1277, 4096 x 5120 468.4 / 468.4.  Nor for 128 x 128 (no change).
-template <typename C>
-__device__ __forceinline__ void product_wide(uint32_t lds0, const GemmArgs &a, int f0, int t0, int wave, int lane,
-                                             f32x4 (&acc)[C::FB][C::TB]) {
+template <typename C, typename Args>
+__device__ __forceinline__ void product_wide(uint32_t lds0, const Args &a, int f0, int t0, int wave, int lane,
+                                             f32x4 (&acc)[C::FB][C::TB], uint32_t table) {
     constexpr int FB = C::FB, TB = C::TB, FH = C::FH, S = C::S, W = C::kWaves;
     const int col = lane % 16, quad = lane / 16;
     const int fw = wave / C::WT, tw = wave % C::WT;
@@ -478,6 +508,16 @@ __device__ __forceinline__ void product_wide(uint32_t lds0, const GemmArgs &a, i
             dst[i] = __builtin_amdgcn_readfirstlane(lds0 + (i < C::kLoadsX ? C::kWBytes : 0) + uint32_t(g) * 1024);
         }
     }
+    // for the present k-tile of the adapters: load i's lane offsets
+    AdapterTilesOf<C, Args> extra(a, f0, t0, table);
+    const uint32_t granule = (lane % 8) ^ swz((wave & 1) * 8 + lane / 8);
+    auto extra_load = [&](int i) {
+        if constexpr (kAdapted<Args>) {
+            const bool is_x = i < C::kLoadsX;
+            const int g = is_x ? wave + i * W : i < C::X ? lo_group(i - C::kLoadsX) : lo_group(i - C::X) + kHalfGroups;
+            load_at_m0(is_x ? extra.t_rsrc : extra.u_rsrc, is_x ? extra.t_offset(g, lane, granule) : extra.u_offset(g, lane, granule), 0);
+        }
+    };
     uint32_t w_addr[2], x_addr[2];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -495,7 +535,10 @@ __device__ __forceinline__ void product_wide(uint32_t lds0, const GemmArgs &a, i
             acc[f][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             asm volatile("" : "+a"(acc[f][t]));
         }
-    const int n_kt = a.d_in / kBK;
+    // four_waves gives it 32 k-tiles at least: those of the adapters are never among the first S
+    const int n_plain = a.d_in / kBK;
+    int n_kt = n_plain;
+    if constexpr (kAdapted<Args>) extra.send(wave, lane);
 #pragma unroll
     for (int p = 0; p < S; ++p)
         if (p < n_kt)
@@ -517,7 +560,8 @@ __device__ __forceinline__ void product_wide(uint32_t lds0, const GemmArgs &a, i
     constexpr int kRest = 2 * PK - PRE, kEveryX = kRest / C::X > 0 ? kRest / C::X : 1, kEveryY = kRest / C::Y > 0 ? kRest / C::Y : 1;
     static_assert(PRE < PK && kRest >= 2 * FH && C::X <= kRest && C::Y <= kRest && PK + TB <= 2 * PK, "everything has its window");
     uint32_t cur = 0;
-    auto tile = [&](int kt, auto left_c) {
+    auto tile = [&](int kt, auto left_c, auto extra_c) {
+        constexpr bool EXTRA = decltype(extra_c)::value;
         constexpr int LEFT = decltype(left_c)::value;
         constexpr bool REFILL = LEFT >= S;
         constexpr int AHEAD = REFILL ? S - 1 : LEFT;
@@ -530,7 +574,8 @@ __device__ __forceinline__ void product_wide(uint32_t lds0, const GemmArgs &a, i
             if constexpr (i == PRE) stage_barrier<AHEAD * N>();
             if constexpr (kLoad) set_m0(dst[j / kEveryX], cur);
             mfma_acc(acc[m][t], lo[m][s], xop[t][s]);
-            if constexpr (kLoad) load_at_m0(j / kEveryX < C::kLoadsX ? x_rsrc : w_rsrc, voff[j / kEveryX], soff);
+            if constexpr (kLoad && EXTRA) extra_load(j / kEveryX);
+            else if constexpr (kLoad) load_at_m0(j / kEveryX < C::kLoadsX ? x_rsrc : w_rsrc, voff[j / kEveryX], soff);
             if constexpr (i < FH) read_lo(i, 1);
             else if constexpr (i < FH + TB) read_x(i - FH, 1);
             if constexpr (j >= 0 && j < 2 * FH) read_hi(j % FH, j / FH);
@@ -544,7 +589,8 @@ __device__ __forceinline__ void product_wide(uint32_t lds0, const GemmArgs &a, i
             if constexpr (i == PRE && LEFT > 0) stage_barrier<(AHEAD - 1) * N + C::Y + (REFILL ? C::X : 0)>();
             if constexpr (kLoad) set_m0(dst[C::X + j / kEveryY], cur);
             mfma_acc(acc[FH + m][t], hi[m][s], xop[t][s]);
-            if constexpr (kLoad) load_at_m0(w_rsrc, voff[C::X + j / kEveryY], soff);
+            if constexpr (kLoad && EXTRA) extra_load(C::X + j / kEveryY);
+            else if constexpr (kLoad) load_at_m0(w_rsrc, voff[C::X + j / kEveryY], soff);
             if constexpr (LEFT > 0) {
                 if constexpr (i < 2) { w_addr[i] += delta; x_addr[i] += delta; }
                 if constexpr (j >= 0 && j < FH) read_lo(j, 0);
@@ -554,10 +600,17 @@ __device__ __forceinline__ void product_wide(uint32_t lds0, const GemmArgs &a, i
         cur = nxt;
     };
     int kt = 0;
-    for (; kt + S < n_kt; ++kt) tile(kt, std::integral_constant<int, S>{});
+    for (; kt + S < n_plain; ++kt) tile(kt, std::integral_constant<int, S>{}, std::false_type{});
+    if constexpr (kAdapted<Args>) {
+        n_kt += extra.look(lane);
+        for (; kt + S < n_kt; ++kt) {
+            extra.next();
+            tile(kt, std::integral_constant<int, S>{}, std::true_type{});
+        }
+    }
     static_for<0, S>([&](auto lc) {
         constexpr int LEFT = S - 1 - decltype(lc)::value;
-        if (kt + LEFT == n_kt - 1) tile(kt++, std::integral_constant<int, LEFT>{});
+        if (kt + LEFT == n_kt - 1) tile(kt++, std::integral_constant<int, LEFT>{}, std::false_type{});
     });
     asm volatile("s_nop 15\n\ts_nop 7");
 #pragma unroll
@@ -581,9 +634,9 @@ __device__ __forceinline__ void product_wide(uint32_t lds0, const GemmArgs &a, i
 // A 64 x 64 tile gains nothing from it (17.4), and operands fetched straight into registers are slower (30).
 //
 // Leaves the wave's own FB x TB blocks in acc, like product().
-template <typename C>
-__device__ __forceinline__ void product_split_k(uint32_t lds0, const GemmArgs &a, int f0, int t0, int wave, int lane,
-                                                f32x4 (&acc)[C::FB][C::TB]) {
+template <typename C, typename Args>
+__device__ __forceinline__ void product_split_k(uint32_t lds0, const Args &a, int f0, int t0, int wave, int lane,
+                                                f32x4 (&acc)[C::FB][C::TB], uint32_t table) {
     constexpr int FB = C::WF * C::FB, TB = C::WT * C::TB, S = C::S, W = C::kWaves, kLoads = C::X + C::Y;
     const int col = lane % 16, quad = lane / 16;
     const int64_t w_rows = min(int64_t(C::kF), int64_t(a.d_out) - f0), x_rows = min(int64_t(C::kT), int64_t(a.n) - t0);
@@ -591,7 +644,7 @@ __device__ __forceinline__ void product_split_k(uint32_t lds0, const GemmArgs &a
         const_cast<__bf16 *>(a.w + int64_t(f0) * a.d_in), 0, int(w_rows * a.d_in * 2), 0x00020000);
     const __amdgpu_buffer_rsrc_t x_rsrc = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<__bf16 *>(a.x + int64_t(t0) * a.d_in), 0, int(x_rows * a.d_in * 2), 0x00020000);
-    const int n_kt = a.d_in / kBK;
+    const int n_plain = a.d_in / kBK;
     // As in product(): a load moves 8 rows, and all of a wave's groups of rows have the parity of the wave.  A k-tile
     // past the last is sent for outside the buffers (nothing is fetched, zeros arrive), which leaves one body
     // for every pair: behind the loads waited for there are always as many others.
@@ -601,10 +654,25 @@ __device__ __forceinline__ void product_split_k(uint32_t lds0, const GemmArgs &a
         const bool is_x = i < C::kLoadsX;
         const int rows8 = wave + (is_x ? i : i - C::kLoadsX) * W;
         load_to_lds_16(is_x ? x_rsrc : w_rsrc, __builtin_amdgcn_readfirstlane(lds0 + stage + (is_x ? C::kWBytes : 0) + rows8 * 1024),
-                       kt < n_kt ? voff : 0x80000000u,
+                       kt < n_plain ? voff : 0x80000000u,
                        __builtin_amdgcn_readfirstlane(uint32_t(kt) * kRowBytes + uint32_t(rows8) * 8 * row_bytes));
     };
     auto load_pair = [&](int i, int kt, uint32_t stage) { load(i % kLoads, kt + i / kLoads, stage + (i / kLoads) * C::kStage); };
+    // the same where a k-tile may be one of the adapters; the loads of a pair come in the order of its k-tiles
+    AdapterTilesOf<C, Args> extra(a, f0, t0, table);
+    const uint32_t granule = (lane % 8) ^ swz((wave & 1) * 8 + lane / 8);
+    auto load_pair_extra = [&](int i, int kt, uint32_t stage) {
+        if constexpr (kAdapted<Args>) {
+            if (kt + i / kLoads < n_plain) return load_pair(i, kt, stage);
+            const int j = i % kLoads;
+            if (j == 0) extra.next();
+            const bool is_x = j < C::kLoadsX;
+            const int rows8 = wave + (is_x ? j : j - C::kLoadsX) * W;
+            load_to_lds_16(is_x ? extra.t_rsrc : extra.u_rsrc,
+                           __builtin_amdgcn_readfirstlane(lds0 + stage + (i / kLoads) * C::kStage + (is_x ? C::kWBytes : 0) + rows8 * 1024),
+                           is_x ? extra.t_offset(rows8, lane, granule) : extra.u_offset(rows8, lane, granule), 0);
+        }
+    };
     // operand addresses of this wave's k-step in the first pair of stages
     const uint32_t w_addr = lds0 + (wave / 2) * C::kStage + col * kRowBytes + 16 * ((4 * (wave % 2) + quad) ^ swz(col));
     const uint32_t x_addr = w_addr + C::kWBytes;
@@ -622,15 +690,27 @@ __device__ __forceinline__ void product_split_k(uint32_t lds0, const GemmArgs &a
     for (int f = 0; f < FB; ++f)
 #pragma unroll
         for (int t = 0; t < TB; ++t) part[f][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    int n_kt = n_plain;
+    if constexpr (kAdapted<Args>) {
+        extra.send(wave, lane);
+        if (n_plain < S) {                               // the adapters' k-tiles are among the first ones sent for
+            stage_barrier<0>();
+            n_kt += extra.look(lane);
+        }
+    }
 #pragma unroll
     for (int p = 0; p < S; p += 2)
 #pragma unroll
-        for (int i = 0; i < 2 * kLoads; ++i) load_pair(i, p, p * C::kStage);
+        for (int i = 0; i < 2 * kLoads; ++i) {
+            if (kAdapted<Args> && n_plain < S) load_pair_extra(i, p, p * C::kStage);
+            else load_pair(i, p, p * C::kStage);
+        }
     stage_barrier<(S - 2) * kLoads>();                   // the first pair has landed
     Operands even, odd;                                  // of the pairs of even and odd number
     read(even, 0);
     uint32_t cur = 0;                                    // first stage of the pair at kt
-    auto pair = [&](int kt, const Operands &now, Operands &next) {
+    auto pair = [&](int kt, const Operands &now, Operands &next, auto extra_c) {
+        constexpr bool EXTRA = decltype(extra_c)::value;
         const uint32_t nxt = cur + 2 * C::kStage == C::kRing ? 0u : cur + 2 * C::kStage;
         stage_barrier<(S - 4) * kLoads>();               // the next pair has landed; every wave has its operands of this one, whose stages are free
         read(next, nxt);
@@ -638,14 +718,26 @@ __device__ __forceinline__ void product_split_k(uint32_t lds0, const GemmArgs &a
             constexpr int f = decltype(fc)::value;
 #pragma unroll
             for (int t = 0; t < TB; ++t) part[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(now.w[f], now.x[t], part[f][t], 0, 0, 0);
-            static_for<f * 2 * kLoads / FB, (f + 1) * 2 * kLoads / FB>([&](auto ic) { load_pair(decltype(ic)::value, kt + S, cur); });
+            static_for<f * 2 * kLoads / FB, (f + 1) * 2 * kLoads / FB>([&](auto ic) {
+                if constexpr (EXTRA) load_pair_extra(decltype(ic)::value, kt + S, cur);
+                else load_pair(decltype(ic)::value, kt + S, cur);
+            });
         });
         cur = nxt;
     };
-    for (int kt = 0;; kt += 4) {
-        pair(kt, even, odd);
+    int kt = 0;
+    using Extra = std::integral_constant<bool, kAdapted<Args>>;
+    if constexpr (kAdapted<Args>) {
+        for (; kt + 2 + S + 1 < n_plain; kt += 4) {
+            pair(kt, even, odd, std::false_type{});
+            pair(kt + 2, odd, even, std::false_type{});
+        }
+        if (n_plain >= S) n_kt += extra.look(lane);
+    }
+    for (;; kt += 4) {
+        pair(kt, even, odd, Extra{});
         if (kt + 2 >= n_kt) break;
-        pair(kt + 2, odd, even);
+        pair(kt + 2, odd, even, Extra{});
         if (kt + 4 >= n_kt) break;
     }
     // every wave's partial tile through LDS; a wave adds up its own blocks, in the order of the waves
@@ -765,7 +857,7 @@ __device__ __forceinline__ void store_tile(uint32_t out_lds, const f32x4 (&acc)[
 // One tile from its first load to its last store.  QKV = true: the epilogue cuts the features into
 // q | k | v sections of heads * HD, normalises and rotates q and k.  QKV = false: plain y = x W^T + b.
 template <bool QKV, int HD, typename C, typename Args>
-__device__ __forceinline__ void run_tile(uint32_t lds0, const Args &a, int f0, int t0) {
+__device__ __forceinline__ void run_tile(uint32_t lds0, const Args &a, int f0, int t0, uint32_t table) {
     constexpr int FB = C::FB, TB = C::TB;
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
@@ -785,11 +877,10 @@ __device__ __forceinline__ void run_tile(uint32_t lds0, const Args &a, int f0, i
         const float *tp = a.rope.turns[tid % kMaxPairs];
         turns_pre = f32x4{tp[0], tp[1], tp[2], 0.0f};
     }
-    static_assert(!kAdapted<Args> || C::HOW == kShared, "the others know nothing of adapters");
     f32x4 acc[FB][TB];
-    if constexpr (C::SPLIT) product_split_k<C>(lds0, a, f0, t0, wave, lane, acc);
-    else if constexpr (C::HOW == kWide) product_wide<C>(lds0, a, f0, t0, wave, lane, acc);
-    else product<C>(lds0, a, f0, t0, wave, lane, acc);
+    if constexpr (C::SPLIT) product_split_k<C>(lds0, a, f0, t0, wave, lane, acc, table);
+    else if constexpr (C::HOW == kWide) product_wide<C>(lds0, a, f0, t0, wave, lane, acc, table);
+    else product<C>(lds0, a, f0, t0, wave, lane, acc, table);
 
     stage_barrier<0>();                                  // the ring is free: every wave has read its last operand
     const uint32_t out_lds = lds0 + wave * (16 * FB * 32), rope_lds = lds0 + C::kOut, ss_lds = rope_lds + kMaxPairs * 16;
@@ -872,6 +963,7 @@ __global__ __launch_bounds__(P::kThreads, P::HOW == kShared ? 2 : 1) void gemm_k
     static_assert(P::kThreads == R::kThreads && P::kF % R::kF == 0 && P::kT % R::kT == 0, "R cuts P");
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const uint32_t lds0 = uint32_t(uintptr_t(LP_LDS_PTR(unsigned char, smem)));
+    const uint32_t table = lds0 + (P::kLds > R::kLds ? P::kLds : R::kLds);       // of the adapters
     constexpr int kCutF = P::kF / R::kF, kCut = kCutF * (P::kT / R::kT);
     const bool cut = std::is_same<P, R>::value ? false : int(blockIdx.x) >= a.whole;
     int tile, part = 0;
@@ -888,10 +980,10 @@ __global__ __launch_bounds__(P::kThreads, P::HOW == kShared ? 2 : 1) void gemm_k
     const int ftile = in_panel / panel_h, ttile = panel * kPanel + in_panel - ftile * panel_h;
     const int f0 = ftile * P::kF, t0 = ttile * P::kT;
     if (!cut) {
-        run_tile<QKV, HD, P>(lds0, a, f0, t0);
+        run_tile<QKV, HD, P>(lds0, a, f0, t0, table);
     } else {
         const int fr = f0 + (part % kCutF) * R::kF, tr = t0 + (part / kCutF) * R::kT;
-        if (fr < a.d_out && tr < a.n) run_tile<QKV, HD, R>(lds0, a, fr, tr);
+        if (fr < a.d_out && tr < a.n) run_tile<QKV, HD, R>(lds0, a, fr, tr, table);
     }
 }
 
@@ -1022,7 +1114,8 @@ Plan pick_plan(int64_t n, int32_t d_in, int32_t d_out, bool small_ok, int cus) {
 
 template <bool QKV, int HD, typename P, typename R, typename Args>
 int launch_tiles(Args a, int64_t whole, hipStream_t stream) {
-    constexpr int kLds = P::kLds > R::kLds ? P::kLds : R::kLds;
+    constexpr int kLds = (P::kLds > R::kLds ? P::kLds : R::kLds) + (kAdapted<Args> ? kTableBytes : 0);
+    static_assert(kLds <= 160 * 1024, "the LDS of a compute unit");
     static std::atomic<uint64_t> attr_set{0};
     const void *kern = reinterpret_cast<const void *>(&gemm_kernel<QKV, HD, P, R, Args>);
     int dev = 0;
@@ -1049,12 +1142,11 @@ constexpr bool small_tilings(int head_dim) { return head_dim <= 64; }
 // Whether lp_linear runs a plan's tiles of 256 features with four wavefronts: see product_wide.
 bool four_waves(const Plan &p, int32_t d_in) { return p.tile <= 1 && d_in / kBK >= (p.tile == 0 && p.cut == kCutNone ? 64 : 32); }
 
-template <bool QKV, int HD>
-int launch_gemm(GemmArgs a, hipStream_t stream) {
+template <bool QKV, int HD, typename Args>
+int launch_plan(const Plan &p, const Args &a, hipStream_t stream) {
     constexpr bool kSmall = small_tilings(QKV ? HD : 0);
-    const int cus = lp::device_compute_units();
-    if (cus <= 0) return LP_ERR_HIP;
-    const Plan p = pick_plan(a.n, a.d_in, a.d_out, kSmall, cus);
+    // two workgroups of 64 x 64 fill a compute unit's LDS: with the adapters' tables a stage less does
+    using Tile64 = std::conditional_t<kAdapted<Args>, Tiling<2, 2, 2, 2, 4>, Tile64x64>;
     if constexpr (!QKV) {
         if (four_waves(p, a.d_in)) {
             switch (p.tile * 8 + p.cut + 1) {
@@ -1075,13 +1167,20 @@ int launch_gemm(GemmArgs a, hipStream_t stream) {
         case 2 * 8: return launch_tiles<QKV, HD, Tile128x128, Tile128x128>(a, p.whole, stream);
         case 3 * 8: return launch_tiles<QKV, HD, Tile128x64, Tile128x64>(a, p.whole, stream);
         case 4 * 8:
-            if constexpr (kSmall) return launch_tiles<QKV, HD, Tile64x64, Tile64x64>(a, p.whole, stream);
+            if constexpr (kSmall) return launch_tiles<QKV, HD, Tile64, Tile64>(a, p.whole, stream);
             [[fallthrough]];
         case 5 * 8:
             if constexpr (kSmall) return launch_tiles<QKV, HD, Split64x32, Split64x32>(a, p.whole, stream);
             [[fallthrough]];
         default: return launch_tiles<QKV, HD, Tile256x256, Tile256x256>(a, p.whole, stream);
     }
+}
+
+template <bool QKV, int HD>
+int launch_gemm(const GemmArgs &a, hipStream_t stream) {
+    const int cus = lp::device_compute_units();
+    if (cus <= 0) return LP_ERR_HIP;
+    return launch_plan<QKV, HD>(pick_plan(a.n, a.d_in, a.d_out, small_tilings(QKV ? HD : 0), cus), a, stream);
 }
 
 // A plan as lp_internal_gemm_way states it.

@@ -96,7 +96,7 @@ def test_linear_adapters_refusals():
                         ((1 << 24, (1 << 25) + 2, 8, 1.0), inv), ((1 << 24, 1 << 25, 8, NAN), inv), ((1 << 24, 1 << 25, 8, INF), inv)):
         assert _linear(adapters=_adapters(bad)) == status
         assert _linear(starts=(0, 3, 3), adapters=_adapters(GOOD, bad)) == status               # of a request without rows too
-    assert _linear(ws=None) == inv and _linear(ws=(1 << 26) + 8) == inv and _linear(size=4224 + 3 * 128 - 1) == inv
+    assert _linear(ws=None) == inv and _linear(ws=(1 << 26) + 8) == inv and _linear(size=3200 + 3 * 128 - 1) == inv
     assert _linear(ws=1 << 20) == inv and _linear(ws=1 << 21) == inv and _linear(ws=1 << 22) == inv
     # nothing to do
     assert _linear(None, None, None, None, (0, 0), ws=None, size=0) == lp.LP_OK and _linear(starts=(), adapters="null") == lp.LP_OK
@@ -104,8 +104,8 @@ def test_linear_adapters_refusals():
 
 def test_workspace_size():
     size = lp._lib().lp_adapter_workspace_size
-    assert size(10, 8, 1) == size(10, 32, 1) == 4224 + 10 * 128 and size(10, 33, 1) == 4224 + 10 * 256
-    assert size(10, 256, 3) == 4224 + 10 * 3 * 8 * 128
+    assert size(10, 8, 1) == size(10, 32, 1) == 3200 + 10 * 128 and size(10, 33, 1) == 3200 + 10 * 256
+    assert size(10, 256, 3) == 3200 + 10 * 3 * 8 * 128
     assert size(0, 8, 1) == 0 and size(10, 0, 3) == 0
     assert size(-1, 8, 1) == size(1, -8, 1) == size(1, 8, 2) == lp.LP_ERR_INVALID_ARG
     assert size(1, 264, 1) == size(2 ** 31 - 1, 8, 1) == lp.LP_ERR_UNSUPPORTED
@@ -133,7 +133,7 @@ def test_qkv_adapters_refusals():
                    (0, rope((-2, -2, 1))), (0, rope((1, 2, 2), base=-1.0))):
         assert _qkv(ropes=fine[:i] + [bad] + fine[i + 1:]) == inv
     assert _qkv(q=1 << 28) == inv and _qkv(v=1 << 20) == inv
-    assert _qkv(ws=None) == inv and _qkv(size=4224 + 10 * 3 * 128 - 1) == inv and _qkv(ws=1 << 27) == inv
+    assert _qkv(ws=None) == inv and _qkv(size=3200 + 10 * 3 * 128 - 1) == inv and _qkv(ws=1 << 27) == inv
     assert _qkv(starts=(0, 0, 0, 0)) == lp.LP_OK
 
 
