@@ -36,7 +36,12 @@ __host__ __device__ int32_t look_parts(int64_t pieces) {
     return int32_t(by_size < kLooks ? by_size : kLooks);
 }
 
-using DownTile = Tiling<2, 2, 2, 1, 8, kSplitK>;         // 64 rows of D x 32 tokens, four wavefronts sharing k
+// Rows of D x tokens.  The four wavefronts share k where there are few tokens, and otherwise the tokens.
+using DownFew = Tiling<2, 2, 2, 1, 8, kSplitK>;          // 64 x 32
+using DownMany = Tiling<1, 4, 4, 2, 6>;                  // 64 x 128
+using DownTall = Tiling<1, 4, 8, 1, 3>;                  // 128 x 64
+constexpr int kDownThreads = 256;
+static_assert(DownFew::kThreads == kDownThreads && DownMany::kThreads == kDownThreads && DownTall::kThreads == kDownThreads, "look_over's too");
 
 // Whether part of a run's U holds an infinity or a NaN, to its word of the control block; the first workgroup writes the rest of the block.
 __device__ void look_over(const DownArgs &a, int wg) {
@@ -49,7 +54,7 @@ __device__ void look_over(const DownArgs &a, int wg) {
     uint32_t bad = 0;
     auto look = [&](uint32_t two) { bad |= uint32_t((two & 0x7f80u) == 0x7f80u) | uint32_t((two & 0x7f800000u) == 0x7f800000u); };
 #pragma unroll 8
-    for (int64_t i = pieces * part / parts + threadIdx.x; i < last; i += DownTile::kThreads) {
+    for (int64_t i = pieces * part / parts + threadIdx.x; i < last; i += kDownThreads) {
         const uint4 p = u[i];
         look(p.x);
         look(p.y);
@@ -68,8 +73,8 @@ __device__ void look_over(const DownArgs &a, int wg) {
     }
 }
 
-__global__ __launch_bounds__(DownTile::kThreads, 1) void adapter_down_kernel(const DownArgs a) {
-    using C = DownTile;
+template <typename C>
+__global__ __launch_bounds__(kDownThreads, 1) void adapter_down_kernel(const DownArgs a) {
     if (int(blockIdx.x) < a.looks) return look_over(a, int(blockIdx.x));
     const int wg = int(blockIdx.x) - a.looks;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
@@ -86,19 +91,24 @@ __global__ __launch_bounds__(DownTile::kThreads, 1) void adapter_down_kernel(con
     g.d_in = a.d_in;
     g.d_out = rows;
     f32x4 acc[C::FB][C::TB];
-    product_split_k<C>(lds0, g, f0, t0, wave, lane, acc, 0);
+    if constexpr (C::SPLIT) product_split_k<C>(lds0, g, f0, t0, wave, lane, acc, 0);
+    else product<C>(lds0, g, f0, t0, wave, lane, acc, 0);
     const float scale = a.run[r].scale;
-    const int tok = t0 + wave % C::WT * 16 + col;
 #pragma unroll
     for (int f = 0; f < C::FB; ++f) {
         const int row = f0 + (wave / C::WT * C::FB + f) * 16 + 4 * quad;   // of D; four of them, of one section
-        if (row >= rows || tok >= g.n) continue;
+        if (row >= rows) break;
         const int section = row / rank, at = row - section * rank;
-        const f32x4 v = acc[f][0] * scale;
-        const bf16x4 hi = __builtin_convertvector(v, bf16x4), lo = __builtin_convertvector(v - __builtin_convertvector(hi, f32x4), bf16x4);
-        __bf16 *to = a.t + int64_t(tok) * (a.t_row / 2) + (section * a.t_blocks + at / kRanks) * (2 * kRanks) + at % kRanks;
-        *reinterpret_cast<bf16x4 *>(to) = hi;
-        *reinterpret_cast<bf16x4 *>(to + kRanks) = lo;
+        __bf16 *to = a.t + (section * a.t_blocks + at / kRanks) * (2 * kRanks) + at % kRanks;
+#pragma unroll
+        for (int t = 0; t < C::TB; ++t) {
+            const int tok = t0 + (wave % C::WT * C::TB + t) * 16 + col;
+            if (tok >= g.n) break;
+            const f32x4 v = acc[f][t] * scale;
+            const bf16x4 hi = __builtin_convertvector(v, bf16x4), lo = __builtin_convertvector(v - __builtin_convertvector(hi, f32x4), bf16x4);
+            *reinterpret_cast<bf16x4 *>(to + int64_t(tok) * (a.t_row / 2)) = hi;
+            *reinterpret_cast<bf16x4 *>(to + int64_t(tok) * (a.t_row / 2) + kRanks) = lo;
+        }
     }
 }
 
@@ -110,7 +120,6 @@ int64_t t_row_bytes(int32_t rank, int32_t sections) { return int64_t(sections) *
 struct Runs {
     RequestTable requests;
     int32_t runs = 0, largest = 0;       // runs; the largest rank
-    int64_t workgroups = 0;              // of the down products
     DownArgs down{};
 };
 
@@ -141,15 +150,6 @@ int make_runs(const lp_requests *requests, const lp_adapter *adapters, int32_t d
     const int32_t n = int32_t(q.rows());
     for (int i = out->runs; i <= LP_MAX_REQUESTS; ++i)
         out->down.run[i] = DownRun{i == out->runs ? n : INT32_MAX, 0, INT32_MAX, INT32_MAX, 0.0f, nullptr, nullptr};
-    for (int i = 0; i < out->runs; ++i) {
-        const int64_t tokens = (int64_t(out->down.run[i + 1].start) - out->down.run[i].start + DownTile::kT - 1) / DownTile::kT;
-        const int64_t rows = (int64_t(sections) * out->down.run[i].rank + DownTile::kF - 1) / DownTile::kF;
-        out->down.run[i].first = int32_t(out->workgroups);
-        out->workgroups += tokens * rows;
-        out->down.run[i].first_look = out->down.looks;
-        out->down.looks += look_parts(int64_t(d_out) * out->down.run[i].rank / 8);
-        if ((out->workgroups + out->down.looks) * DownTile::kThreads > lp::kMaxLaunchThreads) return LP_ERR_UNSUPPORTED;
-    }
     out->down.d_in = d_in;
     out->down.d_out = d_out;
     out->down.sections = sections;
@@ -169,6 +169,48 @@ Plan pick_adapted(int32_t n, int32_t d_in, int32_t d_out, int32_t head_dim, int 
     });
 }
 
+// Workgroups of C that the down products take: the tiles, every one of a single run, behind those that look over U.
+template <typename C>
+int64_t down_tiles(DownArgs &d, int32_t runs) {
+    int64_t tiles = 0;
+    for (int i = 0; i < runs; ++i) {
+        d.run[i].first = int32_t(tiles);
+        tiles += (int64_t(d.run[i + 1].start) - d.run[i].start + C::kT - 1) / C::kT * ((int64_t(d.sections) * d.run[i].rank + C::kF - 1) / C::kF);
+    }
+    return tiles;
+}
+template <typename C>
+int launch_down(DownArgs &d, int32_t runs, int dev, hipStream_t stream) {
+    const int64_t workgroups = d.looks + down_tiles<C>(d, runs);
+    if (workgroups * kDownThreads > lp::kMaxLaunchThreads) return LP_ERR_UNSUPPORTED;
+    static std::atomic<uint64_t> attr_set{0};
+    const void *kern = reinterpret_cast<const void *>(&adapter_down_kernel<C>);
+    const int rc = allow_lds(kern, C::kLds, dev, attr_set);
+    if (rc != LP_OK) return rc;
+    return lp::launch_kernel(kern, dim3(uint32_t(workgroups)), dim3(kDownThreads), C::kLds, stream, d);
+}
+
+// The tile of the down products.  Up to one of 64 x 32 for every compute unit the wavefronts share k: 6 rows of d_in 1536 6.0 us, 977 of 4096 in
+// twelve runs 10.9, with 64 x 128 9.6 and 20.0.  Beyond, x is what binds, and tiles of more tokens read D less often: 22380 x 1536
+// 20.8 us in 64 x 32, 15.7 in 64 x 128, 24570 x 5120 72 and 64 (3.9 TB/s of x).  A run with more than 64 rows of D reads x twice there; with more than three
+// quarters of the tokens in such runs 128 x 64 is faster: 13230 x 5120, 96 rows, 41 us, 45 in 64 x 128; 19052 x 1536, 40 % of them with
+// 96 rows and the others with 48, 27.6 and 23.2.
+int run_down(DownArgs &d, int32_t runs, int dev, int cus, hipStream_t stream) {
+    d.looks = 0;
+    int64_t tokens = 0, passes = 0;
+    for (int i = 0; i < runs; ++i) {
+        d.run[i].first_look = d.looks;
+        d.looks += look_parts(int64_t(d.d_out) * d.run[i].rank / 8);
+        if (d.run[i].rank == 0) continue;
+        const int64_t n = int64_t(d.run[i + 1].start) - d.run[i].start;
+        tokens += n;
+        passes += n * ((d.sections * d.run[i].rank + 63) / 64);
+    }
+    if (down_tiles<DownFew>(d, runs) <= cus) return launch_down<DownFew>(d, runs, dev, stream);
+    if (4 * passes > 7 * tokens) return launch_down<DownTall>(d, runs, dev, stream);
+    return launch_down<DownMany>(d, runs, dev, stream);
+}
+
 // What the calls share from here on: the workspace, the down products, the tilings.
 template <bool QKV, int HD>
 int project(AdaptedArgs<QKV> &a, Runs &runs, void *workspace, int64_t workspace_bytes, hipStream_t stream) {
@@ -184,13 +226,9 @@ int project(AdaptedArgs<QKV> &a, Runs &runs, void *workspace, int64_t workspace_
         d.t = static_cast<__bf16 *>(workspace) + kControlBytes / 2;
         d.t_row = int32_t(t_row);
         d.t_blocks = (runs.largest + kRanks - 1) / kRanks;
-        static std::atomic<uint64_t> attr_set{0};
-        const void *kern = reinterpret_cast<const void *>(&adapter_down_kernel);
-        int rc = allow_lds(kern, DownTile::kLds, dev, attr_set);
+        const int rc = run_down(d, runs.runs, dev, cus, stream);
         if (rc != LP_OK) return rc;
-        rc = lp::launch_kernel(kern, dim3(uint32_t(d.looks + runs.workgroups)), dim3(DownTile::kThreads), DownTile::kLds, stream, d);
-        if (rc != LP_OK) return rc;
-        a.control = d.control;
+    a.control = d.control;
         a.t = d.t;
         a.t_row = d.t_row;
         a.t_blocks = d.t_blocks;
