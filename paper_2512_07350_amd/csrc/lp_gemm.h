@@ -41,7 +41,7 @@ struct RopeArgs {
     float eps;
 };
 
-struct GemmArgs {
+struct GemmHead {
     const __bf16 *x, *w;
     const float *bias;           // [d_out] or nullptr
     __bf16 *out[3];              // plain: out[0] = y [n, d_out]; qkv: q, k, v [n, heads, head_dim]
@@ -49,6 +49,8 @@ struct GemmArgs {
     int32_t n, d_in, d_out;
     int32_t heads;               // qkv: heads; d_out = 3 * heads * head_dim
     int32_t n_ftiles, n_ttiles;  // tiles of the call's tiling
+};
+struct GemmArgs : GemmHead {
     int32_t whole;               // workgroups [0, whole) take one tile each; the tiles from there on are cut in smaller ones
     RopeArgs rope;
 };
@@ -79,11 +81,12 @@ struct AdapterControl {
 constexpr int kControlBytes = sizeof(AdapterControl), kTableBytes = kControlBytes - sizeof(AdapterControl::nan);
 static_assert(kTableBytes == 3 * 1024 && sizeof(AdapterRun) == 32, "whole loads");
 template <bool QKV>
-struct AdaptedArgs : GemmArgs {
+struct AdaptedArgs : GemmHead {
+    int32_t whole;
     // t: row i at i * t_row bytes, per section (q, k, v; one otherwise) t_blocks groups of 32 ranks: 32 values, then what they leave
+    int32_t t_row, t_blocks;
     const __bf16 *t;
     const AdapterControl *control;       // nullptr: no run has an adapter
-    int32_t t_row, t_blocks;
 };
 // QKV: where the tokens of each request are rotated to.
 struct RequestGrid {
@@ -91,6 +94,7 @@ struct RequestGrid {
 };
 template <>
 struct AdaptedArgs<true> : AdaptedArgs<false> {
+    RopeArgs rope;
     int32_t requests;
     RequestGrid grid[LP_MAX_REQUESTS];
 };
@@ -156,20 +160,25 @@ struct AdapterTiles {
     const uint32_t table;                // LDS
     uint64_t left = 0, not_finite = 0;   // runs still to come, the present one included; those whose U is not finite
     int first_section, last_section, section;
-    int block = 0, blocks = 0;           // of the present run
-    uint32_t granules = 0, t_col = 0;    // 16-byte pieces of U's rows; offset of the k-tile in t's
-    uint32_t t_row = 0;                  // bytes from row to row of t; 0: every row is the one of NaN, U is zeros
-    int t_lo = 0, t_hi = 0, f_lo = 0, f_hi = 0;          // rows of the tile that are the run's, features that are the section's
+    // of the present k-tile: 16-byte pieces that U's rows have from it on; offset in U's rows and t's; the run's rows of the tile
+    int pieces = 0;
+    uint32_t u_col = 0, t_col = 0, u_row = 0;            // u_row: pieces of a whole row of U
+    uint32_t t_rows = ~0u;               // 0: every row of t is the one of NaN
+    int t_lo = 0;
+    uint32_t t_count = 0;
+    int f_lo = 0;                        // features of the tile that are the section's
+    uint32_t f_count = 0;
     int32_t start, end, rank;            // of run `lane`
     uint32_t up_lo, up_hi;
-    __amdgpu_buffer_rsrc_t u_rsrc, t_rsrc;
+    __amdgpu_buffer_rsrc_t u_rsrc, t_rsrc, t_all;
 
     __device__ __forceinline__ AdapterTiles(const Args &args, int f, int t, uint32_t table_lds) : a(args), f0(f), t0(t), table(table_lds) {
         const int dm = QKV ? a.d_out / 3 : a.d_out;
         first_section = f0 / dm;
         last_section = min(f0 + C::kF - 1, a.d_out - 1) / dm;
         section = last_section;          // next() turns to the first run
-        u_rsrc = t_rsrc = buffer(nullptr, 0);
+        t_all = buffer(reinterpret_cast<const unsigned char *>(a.t) + int64_t(t0) * a.t_row, int64_t(min(C::kT, a.n - t0)) * a.t_row);
+        u_rsrc = t_rsrc = t_all;
     }
     __device__ __forceinline__ static __amdgpu_buffer_rsrc_t buffer(const void *p, int64_t bytes) {
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, int(bytes), 0x00020000);
@@ -199,54 +208,53 @@ struct AdapterTiles {
         for (uint64_t m = left; m != 0; m &= m - 1) count += __builtin_amdgcn_readlane(tiles, __builtin_ctzll(m));
         return count * (last_section - first_section + 1);
     }
-    // The k-tile behind the present one.  Past the last one: one of zeros.
+    // The k-tile behind the present one.  A wavefront alone on its SIMD takes 5 cycles an instruction here, so that there are few: of
+    // 6 rows of d_in 1536 a k-tile of the adapters took 0.24 us with half as many more.
     __device__ __forceinline__ void next() {
-        if (++block < blocks) {
-            t_col += t_row != 0 ? 4 * kRanks : 0;
+        if (pieces > kRanks / 8) {
+            pieces -= kRanks / 8;
+            u_col += 2 * kRanks;
+            t_col += t_rows & (4 * kRanks);
             return;
         }
-        if (blocks > 0 && section == last_section) left &= left - 1;
-        if (left == 0) {
-            t_hi = f_hi = 0;
-            granules = 0;
-            return;
-        }
+        if (pieces > 0 && section == last_section) left &= left - 1;
         section = section == last_section ? first_section : section + 1;
         const int r = __builtin_ctzll(left);
-        const int ranks = __builtin_amdgcn_readlane(rank, r);
-        blocks = (ranks + kRanks - 1) / kRanks;
-        block = 0;
-        granules = uint32_t(ranks) / 8;
+        const uint32_t ranks = uint32_t(__builtin_amdgcn_readlane(rank, r));
+        u_row = ranks / 8;
+        pieces = int(u_row);
+        u_col = t_col = 0;
         t_lo = max(__builtin_amdgcn_readlane(start, r) - t0, 0);
-        t_hi = min(__builtin_amdgcn_readlane(end, r) - t0, C::kT);
+        t_count = uint32_t(min(__builtin_amdgcn_readlane(end, r) - t0, C::kT) - t_lo);
         const int dm = QKV ? a.d_out / 3 : a.d_out;
-        f_lo = section * dm - f0;
-        f_hi = f_lo + dm;
-        const int64_t t_rows = min(int64_t(C::kT), int64_t(a.n) - t0), u_rows = min(int64_t(C::kF), int64_t(a.d_out) - f0);
+        f_lo = QKV ? section * dm - f0 : 0;
+        f_count = uint32_t(QKV ? dm : C::kF);
+        const uint32_t up[2] = {uint32_t(__builtin_amdgcn_readlane(int(up_lo), r)), uint32_t(__builtin_amdgcn_readlane(int(up_hi), r))};
+        const uint64_t u_at = (uint64_t(up[1]) << 32 | up[0]) + uint64_t(uint32_t(f0)) * (2 * ranks);
+        u_rsrc = buffer(reinterpret_cast<const void *>(u_at), uint32_t(min(C::kF, a.d_out - f0)) * (2 * ranks));
+        if (QKV) t_col = uint32_t(section) * uint32_t(a.t_blocks) * (4 * kRanks);
         if ((not_finite >> r) & 1) {
-            t_row = t_col = 0;
+            t_rows = t_col = 0;
             t_rsrc = buffer(a.control->nan, sizeof(a.control->nan));
             u_rsrc = buffer(nullptr, 0);
         } else {
-            t_row = uint32_t(a.t_row);
-            t_col = uint32_t(section) * uint32_t(a.t_blocks) * (4 * kRanks);
-            t_rsrc = buffer(reinterpret_cast<const unsigned char *>(a.t) + int64_t(t0) * a.t_row, t_rows * a.t_row);
-            const uint64_t up = uint64_t(uint32_t(__builtin_amdgcn_readlane(int(up_hi), r))) << 32 | uint32_t(__builtin_amdgcn_readlane(int(up_lo), r));
-            u_rsrc = buffer(reinterpret_cast<const unsigned char *>(up) + int64_t(f0) * ranks * 2, u_rows * ranks * 2);
+            t_rows = ~0u;
+            t_rsrc = t_all;
         }
     }
     // Where lane `lane` of a load of rows 8 group .. 8 group + 7 fetches its granule g (0 .. 7) from; out of the buffer: zeros
     __device__ __forceinline__ uint32_t t_offset(int group, int lane, uint32_t g) const {
         const int row = 8 * group + lane / 8;
-        const bool in = row >= t_lo && row < t_hi && uint32_t(block) * 4 + g % 4 < granules;
-        return in ? uint32_t(row) * t_row + t_col + 16 * g : 0x80000000u;
+        const bool in = uint32_t(row - t_lo) < t_count && int(g % 4) < pieces;
+        return in ? (uint32_t(row * a.t_row) & t_rows) + (16 * g + t_col) : 0x80000000u;
     }
     __device__ __forceinline__ uint32_t u_offset(int group, int lane, uint32_t g) const {
         const int row = 8 * group + lane / 8;
-        const uint32_t piece = uint32_t(block) * 4 + g % 4;
-        return row >= f_lo && row < f_hi && piece < granules ? (uint32_t(row) * granules + piece) * 16 : 0x80000000u;
+        const bool in = (!QKV || uint32_t(row - f_lo) < f_count) && int(g % 4) < pieces;
+        return in ? __umul24(row, u_row) * 16 + (16 * (g % 4) + u_col) : 0x80000000u;
     }
 };
+
 // What a product without adapters has instead.
 struct NoAdapterTiles {
     template <typename Args>
@@ -342,14 +350,16 @@ __device__ __forceinline__ void product(uint32_t lds0, const Args &a, int f0, in
             for (int i = 0; i < C::X; ++i) load_x(i, p, p * C::kStage);
 #pragma unroll
             for (int i = 0; i < C::Y; ++i) load_y(i, p, p * C::kStage);
-        } else if constexpr (kAdapted<Args>) {
-            if (p < n_kt) {
-                extra.next();
+        }
+    }
+    if constexpr (kAdapted<Args>) {                      // rolled: a tile fetches its instructions from a cold cache
+#pragma unroll 1
+        for (int p = n_plain; p < min(S, n_kt); ++p) {
+            extra.next();
 #pragma unroll
-                for (int i = 0; i < C::X; ++i) load_extra_x(i, p * C::kStage);
+            for (int i = 0; i < C::X; ++i) load_extra_x(i, p * C::kStage);
 #pragma unroll
-                for (int i = 0; i < C::Y; ++i) load_extra_y(i, p * C::kStage);
-            }
+            for (int i = 0; i < C::Y; ++i) load_extra_y(i, p * C::kStage);
         }
     }
     // in registers from here on: zeroed right in front of the first products they would be read a wait state too early
@@ -645,6 +655,7 @@ __device__ __forceinline__ void product_split_k(uint32_t lds0, const Args &a, in
     const __amdgpu_buffer_rsrc_t x_rsrc = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<__bf16 *>(a.x + int64_t(t0) * a.d_in), 0, int(x_rows * a.d_in * 2), 0x00020000);
     const int n_plain = a.d_in / kBK;
+    int n_kt = n_plain;
     // As in product(): a load moves 8 rows, and all of a wave's groups of rows have the parity of the wave.  A k-tile
     // past the last is sent for outside the buffers (nothing is fetched, zeros arrive), which leaves one body
     // for every pair: behind the loads waited for there are always as many others.
@@ -658,19 +669,25 @@ __device__ __forceinline__ void product_split_k(uint32_t lds0, const Args &a, in
                        __builtin_amdgcn_readfirstlane(uint32_t(kt) * kRowBytes + uint32_t(rows8) * 8 * row_bytes));
     };
     auto load_pair = [&](int i, int kt, uint32_t stage) { load(i % kLoads, kt + i / kLoads, stage + (i / kLoads) * C::kStage); };
-    // the same where a k-tile may be one of the adapters; the loads of a pair come in the order of its k-tiles
+    // a whole k-tile that may be one of the adapters
     AdapterTilesOf<C, Args> extra(a, f0, t0, table);
     const uint32_t granule = (lane % 8) ^ swz((wave & 1) * 8 + lane / 8);
-    auto load_pair_extra = [&](int i, int kt, uint32_t stage) {
+    auto load_extra = [&](int kt, uint32_t stage) {
         if constexpr (kAdapted<Args>) {
-            if (kt + i / kLoads < n_plain) return load_pair(i, kt, stage);
-            const int j = i % kLoads;
-            if (j == 0) extra.next();
-            const bool is_x = j < C::kLoadsX;
-            const int rows8 = wave + (is_x ? j : j - C::kLoadsX) * W;
-            load_to_lds_16(is_x ? extra.t_rsrc : extra.u_rsrc,
-                           __builtin_amdgcn_readfirstlane(lds0 + stage + (i / kLoads) * C::kStage + (is_x ? C::kWBytes : 0) + rows8 * 1024),
-                           is_x ? extra.t_offset(rows8, lane, granule) : extra.u_offset(rows8, lane, granule), 0);
+            if (kt < n_plain || kt >= n_kt) {            // past the last: zeros, as in load()
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) load(i, kt, stage);
+                return;
+            }
+            extra.next();
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const bool is_x = i < C::kLoadsX;
+                const int rows8 = wave + (is_x ? i : i - C::kLoadsX) * W;
+                load_to_lds_16(is_x ? extra.t_rsrc : extra.u_rsrc,
+                               __builtin_amdgcn_readfirstlane(lds0 + stage + (is_x ? C::kWBytes : 0) + rows8 * 1024),
+                               is_x ? extra.t_offset(rows8, lane, granule) : extra.u_offset(rows8, lane, granule), 0);
+            }
         }
     };
     // operand addresses of this wave's k-step in the first pair of stages
@@ -690,21 +707,11 @@ __device__ __forceinline__ void product_split_k(uint32_t lds0, const Args &a, in
     for (int f = 0; f < FB; ++f)
 #pragma unroll
         for (int t = 0; t < TB; ++t) part[f][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    int n_kt = n_plain;
-    if constexpr (kAdapted<Args>) {
-        extra.send(wave, lane);
-        if (n_plain < S) {                               // the adapters' k-tiles are among the first ones sent for
-            stage_barrier<0>();
-            n_kt += extra.look(lane);
-        }
-    }
+    if constexpr (kAdapted<Args>) extra.send(wave, lane);
 #pragma unroll
     for (int p = 0; p < S; p += 2)
 #pragma unroll
-        for (int i = 0; i < 2 * kLoads; ++i) {
-            if (kAdapted<Args> && n_plain < S) load_pair_extra(i, p, p * C::kStage);
-            else load_pair(i, p, p * C::kStage);
-        }
+        for (int i = 0; i < 2 * kLoads; ++i) load_pair(i, p, p * C::kStage);
     stage_barrier<(S - 2) * kLoads>();                   // the first pair has landed
     Operands even, odd;                                  // of the pairs of even and odd number
     read(even, 0);
@@ -714,13 +721,16 @@ __device__ __forceinline__ void product_split_k(uint32_t lds0, const Args &a, in
         const uint32_t nxt = cur + 2 * C::kStage == C::kRing ? 0u : cur + 2 * C::kStage;
         stage_barrier<(S - 4) * kLoads>();               // the next pair has landed; every wave has its operands of this one, whose stages are free
         read(next, nxt);
+        if constexpr (EXTRA) {
+#pragma unroll 1
+            for (int i = 0; i < 2; ++i) load_extra(kt + S + i, cur + i * C::kStage);
+        }
         static_for<0, FB>([&](auto fc) {
             constexpr int f = decltype(fc)::value;
 #pragma unroll
             for (int t = 0; t < TB; ++t) part[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(now.w[f], now.x[t], part[f][t], 0, 0, 0);
             static_for<f * 2 * kLoads / FB, (f + 1) * 2 * kLoads / FB>([&](auto ic) {
-                if constexpr (EXTRA) load_pair_extra(decltype(ic)::value, kt + S, cur);
-                else load_pair(decltype(ic)::value, kt + S, cur);
+                if constexpr (!EXTRA) load_pair(decltype(ic)::value, kt + S, cur);
             });
         });
         cur = nxt;
@@ -732,7 +742,9 @@ __device__ __forceinline__ void product_split_k(uint32_t lds0, const Args &a, in
             pair(kt, even, odd, std::false_type{});
             pair(kt + 2, odd, even, std::false_type{});
         }
-        if (n_plain >= S) n_kt += extra.look(lane);
+        // the adapters' k-tiles come behind the first S, those past the last of x and W among these being zeros
+        const int count = extra.look(lane);
+        if (count > 0) n_kt = max(n_plain, S) + count;
     }
     for (;; kt += 4) {
         pair(kt, even, odd, Extra{});
@@ -872,7 +884,7 @@ __device__ __forceinline__ void run_tile(uint32_t lds0, const Args &a, int f0, i
     f32x2 bias_pre = {0.0f, 0.0f}, gain_pre = {0.0f, 0.0f};
     f32x4 turns_pre = {0.0f, 0.0f, 0.0f, 0.0f};
     if (live && a.bias != nullptr) bias_pre = *reinterpret_cast<const f32x2 *>(a.bias + fbase + f_pre);
-    if (QKV) {
+    if constexpr (QKV) {
         if (live && section < 2) gain_pre = *reinterpret_cast<const f32x2 *>(a.gain[section] + f_in_section + f_pre);
         const float *tp = a.rope.turns[tid % kMaxPairs];
         turns_pre = f32x4{tp[0], tp[1], tp[2], 0.0f};
@@ -964,6 +976,10 @@ __global__ __launch_bounds__(P::kThreads, P::HOW == kShared ? 2 : 1) void gemm_k
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const uint32_t lds0 = uint32_t(uintptr_t(LP_LDS_PTR(unsigned char, smem)));
     const uint32_t table = lds0 + (P::kLds > R::kLds ? P::kLds : R::kLds);       // of the adapters
+    // Arguments lie in memory that no cache holds yet: all that a tile starts with is sent for at once, not where each is first used
+    if constexpr (kAdapted<Args>)
+        asm volatile("" ::"s"(a.x), "s"(a.w), "s"(a.bias), "s"(a.n), "s"(a.d_in), "s"(a.d_out), "s"(a.n_ftiles), "s"(a.n_ttiles), "s"(a.whole), "s"(a.t),
+                     "s"(a.control), "s"(a.t_row), "s"(a.t_blocks));
     constexpr int kCutF = P::kF / R::kF, kCut = kCutF * (P::kT / R::kT);
     const bool cut = std::is_same<P, R>::value ? false : int(blockIdx.x) >= a.whole;
     int tile, part = 0;
