@@ -16,7 +16,8 @@
  * With classifier-free guidance every sub-latent is denoised twice per step
  * (Eq. 4); lp_attention_batch serves the pair in one launch and
  * lp_reconstruct_guided_step folds guidance, reconstruction and the sampler's
- * update (Eq. 4-6) into one pass.
+ * update (Eq. 4-6) into one pass.  The DiT block's other calls on the tokens of
+ * one sub-latent, and on those of several requests at once (lp_requests), follow.
  *
  * Conventions
  *  - Every call returns an int status: LP_OK (0) or a negative LP_ERR_* code;
@@ -389,7 +390,8 @@ typedef struct lp_modulation {
  * element type is taken; with d and all strides multiples of 8 and 16-byte aligned addresses
  * (modulation included, its stride a multiple of 4) rows move in 16-byte pieces.
  * Mean and variance are binary32 sums over the row held in registers, the variance about the mean; one rounding, on
- * store.  A row that holds an infinity or a NaN comes out unspecified, other rows are not affected.
+ * store.  A row that holds an infinity, a NaN or values whose squares do not fit binary32 (past 1e18 or so) comes out
+ * unspecified, other rows are not affected.
  */
 int lp_norm_modulate(const void *x, int32_t x_type, void *y, const lp_requests *requests, int32_t d, int64_t stride_x,
                      int64_t stride_y, const lp_norm *norm, const lp_modulation *modulation, void *stream);

@@ -192,23 +192,31 @@ int launch_down(DownArgs &d, int32_t runs, int dev, hipStream_t stream) {
 
 // The tile of the down products.  Up to one of 64 x 32 for every compute unit the wavefronts share k: 6 rows of d_in 1536 6.0 us, 977 of 4096 in
 // twelve runs 10.9, with 64 x 128 9.6 and 20.0.  Beyond, x is what binds, and tiles of more tokens read D less often: 22380 x 1536
-// 20.8 us in 64 x 32, 15.7 in 64 x 128, 24570 x 5120 72 and 64 (3.9 TB/s of x).  A run with more than 64 rows of D reads x twice there; with more than three
-// quarters of the tokens in such runs 128 x 64 is faster: 13230 x 5120, 96 rows, 41 us, 45 in 64 x 128; 19052 x 1536, 40 % of them with
-// 96 rows and the others with 48, 27.6 and 23.2.
-int run_down(DownArgs &d, int32_t runs, int dev, int cus, hipStream_t stream) {
-    d.looks = 0;
+// 20.8 us in 64 x 32, 15.7 in 64 x 128 (4.4 TB/s of x), 24570 x 5120 72 and 64 (3.9).  A run with more than 64 rows of D reads x twice there; with more
+// than three quarters of the tokens in such runs 128 x 64 is faster: 13230 x 5120, 96 rows, 41 us, 45 in 64 x 128; 19052 x 1536, 40 % of
+// them with 96 rows and the others with 48, 27.6 and 23.2.
+enum Down { kDownFew, kDownMany, kDownTall };
+Down pick_down(DownArgs &d, int32_t runs, int cus) {
     int64_t tokens = 0, passes = 0;
     for (int i = 0; i < runs; ++i) {
-        d.run[i].first_look = d.looks;
-        d.looks += look_parts(int64_t(d.d_out) * d.run[i].rank / 8);
         if (d.run[i].rank == 0) continue;
         const int64_t n = int64_t(d.run[i + 1].start) - d.run[i].start;
         tokens += n;
         passes += n * ((d.sections * d.run[i].rank + 63) / 64);
     }
-    if (down_tiles<DownFew>(d, runs) <= cus) return launch_down<DownFew>(d, runs, dev, stream);
-    if (4 * passes > 7 * tokens) return launch_down<DownTall>(d, runs, dev, stream);
-    return launch_down<DownMany>(d, runs, dev, stream);
+    return down_tiles<DownFew>(d, runs) <= cus ? kDownFew : 4 * passes > 7 * tokens ? kDownTall : kDownMany;
+}
+int run_down(DownArgs &d, int32_t runs, int dev, int cus, hipStream_t stream) {
+    d.looks = 0;
+    for (int i = 0; i < runs; ++i) {
+        d.run[i].first_look = d.looks;
+        d.looks += look_parts(int64_t(d.d_out) * d.run[i].rank / 8);
+    }
+    switch (pick_down(d, runs, cus)) {
+        case kDownFew: return launch_down<DownFew>(d, runs, dev, stream);
+        case kDownTall: return launch_down<DownTall>(d, runs, dev, stream);
+        default: return launch_down<DownMany>(d, runs, dev, stream);
+    }
 }
 
 // What the calls share from here on: the workspace, the down products, the tilings.
@@ -238,17 +246,21 @@ int project(AdaptedArgs<QKV> &a, Runs &runs, void *workspace, int64_t workspace_
 
 }  // namespace
 
-// For the tests, as lp_internal_gemm_way: rows and ranks of the requests.
+// For the tests, as lp_internal_gemm_way: rows and ranks of the requests; way[6], way[7]: rows of D and tokens of the down products' tile.
 extern "C" int lp_internal_adapted_way(const int64_t *start, const int32_t *rank, int32_t count, int32_t d_in, int32_t d_out, int32_t head_dim,
-                                       int32_t cus, int64_t way[6]) {
-    DownRun run[LP_MAX_REQUESTS + 1];
+                                       int32_t cus, int64_t way[8]) {
+    DownArgs d{};
+    d.sections = head_dim == 0 ? 1 : 3;
     int runs = 0;
     for (int r = 0; r < count; ++r)
-        if (start[r + 1] > start[r]) run[runs++] = DownRun{int32_t(start[r]), rank[r], 0, 0, 0.0f, nullptr, nullptr};
-    run[runs] = DownRun{int32_t(start[count]), 0, 0, 0, 0.0f, nullptr, nullptr};
+        if (start[r + 1] > start[r]) d.run[runs++] = DownRun{int32_t(start[r]), rank[r], 0, 0, 0.0f, nullptr, nullptr};
+    d.run[runs] = DownRun{int32_t(start[count]), 0, 0, 0, 0.0f, nullptr, nullptr};
     const int64_t n = start[count];
-    const Plan p = pick_adapted(int32_t(n), d_in, d_out, head_dim, cus, runs, run);
+    const Plan p = pick_adapted(int32_t(n), d_in, d_out, head_dim, cus, runs, d.run);
     plan_way(p, n, d_out, head_dim == 0 && four_waves(p, d_in), way);
+    const Down down = pick_down(d, runs, cus);
+    way[6] = down == kDownFew ? DownFew::kF : down == kDownMany ? DownMany::kF : DownTall::kF;
+    way[7] = down == kDownFew ? DownFew::kT : down == kDownMany ? DownMany::kT : DownTall::kT;
     return LP_OK;
 }
 

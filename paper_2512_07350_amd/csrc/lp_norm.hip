@@ -344,6 +344,7 @@ extern "C" int lp_norm_modulate(const void *x, int32_t x_type, void *y, const lp
     a.stride_x = stride_x;
     a.stride_y = stride_y;
     a.post = kNone;
+    a.gate = nullptr;
     const bool vec = vectors_aligned(a) && aligned16(x) && aligned16(y) && stride_x % 8 == 0 && stride_y % 8 == 0;
     return run(a, vec, x_type == LP_F32, false, static_cast<hipStream_t>(stream));
 }

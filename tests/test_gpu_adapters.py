@@ -21,14 +21,14 @@ pytestmark = pytest.mark.gpu
 EPS = 1e-6
 
 
-def way(lengths, ranks, d_in, d_out, head_dim=0):
-    """What a call runs: routes.GemmWay."""
+def way(lengths, ranks, d_in, d_out, head_dim=0, cus=None):
+    """What a call runs: routes.GemmWay, and the tile of the down products."""
     fn = lp._lib().lp_internal_adapted_way
     fn.argtypes = [C.POINTER(C.c_int64), C.POINTER(C.c_int32), C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int64)]
     starts = np.concatenate([[0], np.cumsum(lengths)]).tolist()
-    out = (C.c_int64 * 6)()
-    assert fn((C.c_int64 * len(starts))(*starts), (C.c_int32 * len(ranks))(*ranks), len(ranks), d_in, d_out, head_dim, routes._cus(None), out) == 0
-    return routes.GemmWay((out[0], out[1]), (out[2], out[3]) if out[2] else None, out[4], out[5])
+    out = (C.c_int64 * 8)()
+    assert fn((C.c_int64 * len(starts))(*starts), (C.c_int32 * len(ranks))(*ranks), len(ranks), d_in, d_out, head_dim, routes._cus(cus), out) == 0
+    return routes.GemmWay((out[0], out[1]), (out[2], out[3]) if out[2] else None, out[4], out[5]), (out[6], out[7])
 
 
 class Case:
@@ -110,6 +110,10 @@ def test_linear_adapters(lengths, ranks, d_in, d_out):
 
 
 TILINGS = [
+    # wavefronts that share k (3 and 9 k-tiles, fewer and more than its 8 stages, 17 and 30), 64 x 64, four wavefronts to 256 features
+    (40, 192, 640, "64x32"), (77, 576, 896, "64x32"), (33, 1088, 384, "64x32"), (95, 1920, 256, "64x32"), (150, 64, 1152, "64x64"), (200, 320, 2048, "64x64"),
+    (4033, 2112, 1536, "256x128"), (2560, 4096, 6144, "256x256"), (4097, 2112, 4224, "256x256+128x128"), (4353, 2112, 4096, "256x256+128x64"),
+    (6145, 2176, 3584, "256x256+256x128"),
     (66, 64, 8448, "128x64"), (1438, 1024, 1152, "128x64"), (1345, 576, 1536, "128x128"), (75077, 64, 128, "128x128+128x64"),
     (12001, 1024, 384, "256x128"), (3783, 128, 3840, "256x256"), (3600, 128, 4608, "256x256+128x64"), (4097, 1024, 4608, "256x256+128x128"),
     (3601, 512, 6144, "256x256+256x128"),
@@ -122,13 +126,31 @@ def test_linear_adapters_of_every_tiling(n, d_in, d_out, tiles):
     lengths = [n // 3 + 5, n // 4, n // 5, 0]
     lengths[3] = n - sum(lengths)
     ranks = [32, 0, 16, 32]
-    assert str(way(lengths, ranks, d_in, d_out)) == tiles
+    assert str(way(lengths, ranks, d_in, d_out)[0]) == tiles
     c = Case(lengths, ranks, d_in, d_out)
     y = c.linear()
     edges = [s + i for s in c.starts for i in (-2, -1, 0, 1) if 0 <= s + i < n]
     import torch
     rows = torch.tensor(sorted(set(edges + list(range(0, n, max(1, n // 400))) + list(range(min(n, 40))))), device="cuda")
     inside(y[rows], *c.want(rows), tiles)
+    assert torch.isfinite(y.float()).all()
+
+
+@pytest.mark.parametrize("d_in", [64, 192, 1088, 2112])
+@pytest.mark.parametrize("lengths,ranks,tile", [
+    ([40, 1, 33], [8, 72, 256], (64, 32)),
+    ([9000, 77, 3], [16, 72, 64], (64, 128)), ([3000, 0, 6000, 130], [64, 8, 40, 0], (64, 128)),
+    ([3000, 2501], [128, 96], (128, 64)), ([65, 4000, 63], [200, 136, 8], (128, 64)),
+])
+def test_down_products_of_every_tile(lengths, ranks, tile, d_in):
+    """t itself: W and the bias are zero, so that nothing but the adapters is in y."""
+    import torch
+    assert way(lengths, ranks, d_in, 128)[1] == tile
+    c = Case(lengths, ranks, d_in, 128, bias=False)
+    c.w.zero_()
+    y = c.linear()
+    rows = torch.tensor(sorted(set(list(range(0, c.n, max(1, c.n // 700))) + [s + i for s in c.starts for i in range(-3, 3) if 0 <= s + i < c.n])), device="cuda")
+    inside(y[rows], *c.want(rows))
     assert torch.isfinite(y.float()).all()
 
 
@@ -251,6 +273,7 @@ def test_qkv_adapters(grids, ranks, heads, hd):
 
 
 @pytest.mark.parametrize("heads,hd,grid,tiles", [
+    (8, 64, (3, 5, 9), "64x32"), (20, 64, (3, 3, 11), "64x32"), (2, 64, (3, 6, 6), "64x64"), (4, 64, (9, 11, 13), "64x64"),
     (2, 64, (3, 23, 39), "128x64"), (8, 128, (3, 5, 9), "128x64"), (1, 128, (1, 5, 5), "128x64"), (16, 64, (3, 13, 17), "128x128"),
     (8, 128, (3, 20, 20), "128x128"), (36, 128, (6, 10, 10), "128x128+128x64"), (8, 64, (23, 13, 9), "256x128"), (4, 128, (9, 23, 13), "256x128"),
     (8, 64, (11, 33, 15), "256x256"), (10, 128, (7, 23, 23), "256x256"), (6, 64, (22, 18, 33), "256x256+128x64"),
@@ -263,7 +286,7 @@ def test_qkv_adapters_of_every_tiling(heads, hd, grid, tiles):
     t = grid[0]
     grids = [(a,) + grid[1:] for a in (t - t // 2 - t // 3, t // 3, t // 2)]
     c = Qkv(grids, [32, 0, 16], heads, hd)
-    assert str(way(c.lengths, c.ranks, c.d_in, c.d_out, hd)) == tiles
+    assert str(way(c.lengths, c.ranks, c.d_in, c.d_out, hd)[0]) == tiles
     edges = [s + i for s in c.starts for i in (-2, -1, 0, 1) if 0 <= s + i < c.n]
     c.check(torch.tensor(sorted(set(edges + list(range(0, c.n, max(1, c.n // 150))))), device="cuda"))
 
