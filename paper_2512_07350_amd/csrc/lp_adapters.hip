@@ -3,13 +3,13 @@
 //   lp_linear_adapters           y = x W^T + b + s_r (x D_r^T) U_r^T
 //   lp_qkv_projection_adapters   the same in the sections q | k | v, q and k normalised and rotated
 //
-// with r the request that a row belongs to.  Two launches: adapter_down_kernel forms t = s_r x D_r^T of the rows that have an
+// with r the request that a row belongs to.  Two launches (one for few rows, few_down of lp_gemm.h): adapter_down_kernel forms t = s_r x D_r^T of the rows that have an
 // adapter (and looks over every U_r), and the product of lp_gemm.h takes t and U_r as further k-tiles.  The second thus costs a k-tile of 64 for every
 // 32 ranks beside d_in / 64 of them, and no pass over y.
 //
 // What bounds it.  Large calls: the shared product; 24570 x 5120 -> 5120 with ranks 64 and 16 966 us, 900 without adapters, 64 of the
-// difference for t, which reads x once more (3.9 TB/s).  q | k | v of 13230 x 5120, rank 32, 1557 and 1506, 41 for t.  Few rows: two launches, 6 rows of
-// d_in 1536 5.3 + 7.8 us, 5.4 without adapters.
+// difference for t, which reads x once more (3.9 TB/s).  q | k | v of 13230 x 5120, rank 32, 1557 and 1506, 41 for t.  Few rows and ranks: one
+// launch (few_down); with more ranks two, 6 rows of d_in 1536 and rank 128 13.3 us, 5.4 without adapters.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -223,6 +223,26 @@ int run_down(DownArgs &d, int32_t runs, int dev, int cus, hipStream_t stream) {
     }
 }
 
+// Whether a call is taken in one launch (few_down): one round of 64 x 32 tiles at most, and ranks for one product of 64 rows.
+bool takes_few(int64_t n, int32_t d_out, int32_t head_dim, int cus, int32_t runs, const DownRun *run) {
+    if (!small_tilings(head_dim) || (n + Split64x32::kT - 1) / Split64x32::kT * ((d_out + Split64x32::kF - 1) / Split64x32::kF) > cus) return false;
+    int ranks = 0;
+    for (int i = 0; i < runs; ++i) ranks += run[i].rank;
+    return ranks > 0 && ranks <= kFewRanks;              // of 8 each at least: no more than kFewRuns
+}
+template <bool QKV, int HD>
+int launch_few(const AdaptedArgs<QKV> &a, const DownArgs &d, int32_t runs, hipStream_t stream) {
+    FewArgs<QKV> few{};
+    static_cast<AdaptedArgs<QKV> &>(few) = a;
+    for (int i = 0; i < runs; ++i) {
+        if (d.run[i].rank == 0) continue;
+        few.few[few.runs++] = FewRun{d.run[i].down, d.run[i].up, d.run[i].start, d.run[i + 1].start, d.run[i].rank, few.ranks, d.run[i].scale, {0, 0, 0}};
+        few.ranks += d.run[i].rank;
+    }
+    const int64_t tiles = (int64_t(a.n) + Split64x32::kT - 1) / Split64x32::kT * ((a.d_out + Split64x32::kF - 1) / Split64x32::kF);
+    return launch_tiles<QKV, HD, Split64x32, Split64x32>(few, tiles, stream);
+}
+
 // What the calls share from here on: the workspace, the down products, the tilings.
 template <bool QKV, int HD>
 int project(AdaptedArgs<QKV> &a, Runs &runs, void *workspace, int64_t workspace_bytes, hipStream_t stream) {
@@ -232,6 +252,8 @@ int project(AdaptedArgs<QKV> &a, Runs &runs, void *workspace, int64_t workspace_
     const int cus = lp::device_compute_units(&dev);
     if (cus <= 0) return LP_ERR_HIP;
     DownArgs &d = runs.down;
+    if constexpr (small_tilings(QKV ? HD : 0))
+        if (takes_few(a.n, a.d_out, QKV ? HD : 0, cus, runs.runs, d.run)) return launch_few<QKV, HD>(a, d, runs.runs, stream);
     if (runs.largest > 0) {
         d.x = a.x;
         d.control = static_cast<AdapterControl *>(workspace);
@@ -250,7 +272,7 @@ int project(AdaptedArgs<QKV> &a, Runs &runs, void *workspace, int64_t workspace_
 
 }  // namespace
 
-// For the tests, as lp_internal_gemm_way: rows and ranks of the requests; way[6], way[7]: rows of D and tokens of the down products' tile.
+// For the tests, as lp_internal_gemm_way: rows and ranks of the requests; way[6], way[7]: rows of D and tokens of the down products' tile (0, 0: one launch).
 extern "C" int lp_internal_adapted_way(const int64_t *start, const int32_t *rank, int32_t count, int32_t d_in, int32_t d_out, int32_t head_dim,
                                        int32_t cus, int64_t way[8]) {
     DownArgs d{};
@@ -262,6 +284,14 @@ extern "C" int lp_internal_adapted_way(const int64_t *start, const int32_t *rank
     const int64_t n = start[count];
     const Plan p = pick_adapted(int32_t(n), d_in, d_out, head_dim, cus, runs, d.run);
     plan_way(p, n, d_out, head_dim == 0 && four_waves(p, d_in), way);
+    if (takes_few(n, d_out, head_dim, cus, runs, d.run)) {
+        way[0] = Split64x32::kF;
+        way[1] = Split64x32::kT;
+        way[2] = way[3] = way[6] = way[7] = 0;
+        way[4] = (n + Split64x32::kT - 1) / Split64x32::kT * ((d_out + Split64x32::kF - 1) / Split64x32::kF);
+        way[5] = Split64x32::kThreads;
+        return LP_OK;
+    }
     const Down down = pick_down(d, runs, cus);
     way[6] = down == kDownFew ? DownFew::kF : down == kDownMany ? DownMany::kF : DownTall::kF;
     way[7] = down == kDownFew ? DownFew::kT : down == kDownMany ? DownMany::kT : DownTall::kT;
@@ -332,9 +362,8 @@ extern "C" int lp_qkv_projection_adapters(const void *x, const void *w_qkv, cons
             first = r;
             if ((rc = make_rope_args(&ropes[r], rows, head_dim, eps, &a.rope)) != LP_OK) return rc;
         }
-        RopeArgs unused;
         const lp_rope &o = ropes[r];
-        if ((rc = make_rope_args(&o, rows, head_dim, eps, &unused)) != LP_OK) return rc;
+        if ((rc = check_rope(&o, rows, head_dim, eps)) != LP_OK) return rc;
         if (o.base != ropes[first].base) return LP_ERR_INVALID_ARG;
         for (int ax = 0; ax < 3; ++ax)
             if (o.split[ax] != ropes[first].split[ax]) return LP_ERR_INVALID_ARG;

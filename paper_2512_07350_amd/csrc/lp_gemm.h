@@ -98,8 +98,30 @@ struct AdaptedArgs<true> : AdaptedArgs<false> {
     int32_t requests;
     RequestGrid grid[LP_MAX_REQUESTS];
 };
+// Few rows and few ranks: the whole in one launch, see few_down.
+constexpr int kFewRuns = 8, kFewRanks = 64;
+struct FewRun {
+    const __bf16 *down, *up;
+    int32_t start, end, rank;
+    int32_t first;               // its place among the ranks of all runs
+    float scale;
+    int32_t unused[3];
+};
+template <bool QKV>
+struct FewArgs : AdaptedArgs<QKV> {
+    int32_t runs, ranks;
+    alignas(16) FewRun few[kFewRuns];    // past the last: rank 0
+};
 template <typename Args>
-constexpr bool kAdapted = std::is_base_of<AdaptedArgs<false>, Args>::value;
+constexpr bool kFew = std::is_base_of<FewArgs<false>, Args>::value || std::is_base_of<FewArgs<true>, Args>::value;
+template <typename Args>
+constexpr bool kAdapted = std::is_base_of<AdaptedArgs<false>, Args>::value && !kFew<Args>;       // takes adapters as k-tiles
+template <typename Args>
+constexpr bool kGrids = std::is_base_of<AdaptedArgs<true>, Args>::value;                         // every request has its grid
+// A product whose W is made of groups of 8 rows that lie anywhere: those that a wavefront loads (product_split_k)
+struct GroupedArgs : GemmHead {
+    __amdgpu_buffer_rsrc_t group[2];
+};
 
 // granule XOR mask of a tile row (reader and writer use the same function): with 128-byte rows
 // the 16-byte granule g of row r lives at position g ^ swz(r), which makes the ds_read_b128 of
@@ -664,6 +686,14 @@ __device__ __forceinline__ void product_split_k(uint32_t lds0, const Args &a, in
     auto load = [&](int i, int kt, uint32_t stage) {
         const bool is_x = i < C::kLoadsX;
         const int rows8 = wave + (is_x ? i : i - C::kLoadsX) * W;
+        if constexpr (std::is_same<Args, GroupedArgs>::value) {
+            static_assert(C::kF == 16 * W, "two groups to a wave");
+            if (!is_x) {
+                load_to_lds_16(a.group[i - C::kLoadsX], __builtin_amdgcn_readfirstlane(lds0 + stage + rows8 * 1024), kt < n_plain ? voff : 0x80000000u,
+                               __builtin_amdgcn_readfirstlane(uint32_t(kt) * kRowBytes));
+                return;
+            }
+        }
         load_to_lds_16(is_x ? x_rsrc : w_rsrc, __builtin_amdgcn_readfirstlane(lds0 + stage + (is_x ? C::kWBytes : 0) + rows8 * 1024),
                        kt < n_plain ? voff : 0x80000000u,
                        __builtin_amdgcn_readfirstlane(uint32_t(kt) * kRowBytes + uint32_t(rows8) * 8 * row_bytes));
@@ -771,6 +801,133 @@ __device__ __forceinline__ void product_split_k(uint32_t lds0, const Args &a, in
         }
 }
 
+// Calls of few rows in one launch.  Every workgroup of 64 features x 32 tokens forms t of its tokens itself, for the ranks of all runs one after
+// the other (at most 64, so that one more product of 64 rows does: those of the D's, a group of 8 rows to a load), and adds
+//   sum_j U[feature, j] (hi + lo)[token, j]
+// to its product.  t is zero where the token is not of j's run.  It costs the k-tiles of x a second time, in every workgroup, and saves the launch
+// in front and the trip through memory.
+//
+// LDS at `few`: t as kFewRanks / 32 times hi and lo, 32 tokens of 32 ranks; U as 64 features of 32 ranks; the runs whose U is not finite.
+constexpr int kFewT = 0, kFewU = 8192, kFewBad = 16384, kFewBytes = 16384 + 64;
+
+// The runs, one to a lane (the first kFewRuns): fetched in front of the product and looked at behind it, where they have long arrived.
+struct FewTable {
+    u32x4 where;                         // down, up
+    u32x4 rows;                          // start, end, rank, first
+    float scale;
+    __device__ __forceinline__ explicit FewTable(const FewRun *few, int lane) {
+        const FewRun &run = few[lane % kFewRuns];
+        where = *reinterpret_cast<const u32x4 *>(&run.down);
+        rows = *reinterpret_cast<const u32x4 *>(&run.start);
+        scale = run.scale;
+    }
+    __device__ __forceinline__ int get(int i, int r) const { return __builtin_amdgcn_readlane(int(rows[i]), r); }
+    __device__ __forceinline__ const __bf16 *pointer(int i, int r) const {
+        return reinterpret_cast<const __bf16 *>(uint64_t(uint32_t(__builtin_amdgcn_readlane(int(where[2 * i + 1]), r))) << 32 |
+                                                uint32_t(__builtin_amdgcn_readlane(int(where[2 * i]), r)));
+    }
+};
+
+template <typename C, typename Args>
+__device__ __forceinline__ void few_down(uint32_t lds0, uint32_t few, const Args &a, const FewTable &table, int f0, int t0, int wave, int lane) {
+    static_assert(C::SPLIT && C::kF == 64 && C::kT == 32 && C::kWaves == 4, "the layouts here");
+    const int col = lane % 16, quad = lane / 16, tid = threadIdx.x;
+    const int section = kGrids<Args> ? f0 / (a.d_out / 3) : 0;
+    GroupedArgs g{};
+    g.x = g.w = a.x;                                     // in w's place: the groups
+    g.n = a.n;
+    g.d_in = a.d_in;
+    g.d_out = a.d_out;
+    // U: 64 features x 8 pieces of 8 ranks, two to a thread
+    const int j_piece = tid % 8 * 8;
+    const __bf16 *from_d[2] = {a.x, a.x}, *from_u = nullptr;
+    int bytes[2] = {0, 0}, run_of = -1, u_rank = 0;
+    for (int r = 0; r < a.runs; ++r) {
+        const int start = table.get(0, r), end = table.get(1, r), rank = table.get(2, r), first = table.get(3, r);
+        if (j_piece >= first && j_piece < first + rank) {
+            run_of = r;
+            u_rank = rank;
+            from_u = table.pointer(1, r) + (j_piece - first);
+        }
+        if (start < t0 + C::kT && end > t0) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int j = 8 * (wave + 4 * i);
+                if (j >= first && j < first + rank) {
+                    from_d[i] = table.pointer(0, r) + int64_t(section * rank + j - first) * a.d_in;
+                    bytes[i] = 16 * a.d_in;
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) g.group[i] = __builtin_amdgcn_make_buffer_rsrc(const_cast<__bf16 *>(from_d[i]), 0, bytes[i], 0x00020000);
+    u32x4 piece[2] = {};
+    if (from_u != nullptr)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) piece[h] = *reinterpret_cast<const u32x4 *>(from_u + int64_t(f0 + tid / 8 + 32 * h) * u_rank);
+    f32x4 acc[C::FB][C::TB];
+    product_split_k<C>(lds0, g, 0, t0, wave, lane, acc, 0);
+    uint32_t bad = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if ((piece[h][i] & 0x7f80u) == 0x7f80u || (piece[h][i] & 0x7f800000u) == 0x7f800000u) bad = 1u << run_of;
+    // of the wave: a lane's run is one of eight, so that a vote for each does
+    uint32_t words = 0;
+    for (int r = 0; r < a.runs; ++r) words |= __ballot(bad == 1u << r) != 0 ? 1u << r : 0u;
+    if (lane == 0) lds_store<uint32_t>(few + kFewBad + 4 * wave, words);
+    __syncthreads();
+    const u32x4 all = lds_load<u32x4>(few + kFewBad);
+    bad = __builtin_amdgcn_readfirstlane(all.x | all.y | all.z | all.w);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        if (run_of >= 0 && ((bad >> run_of) & 1)) piece[h] = u32x4{0, 0, 0, 0};
+        lds_store<u32x4>(few + kFewU + j_piece / kRanks * 4096 + (tid / 8 + 32 * h) * 64 + j_piece % kRanks * 2, piece[h]);
+    }
+    const int tok = wave % 2 * 16 + col;
+    f32x4 v[C::FB] = {};
+    for (int r = 0; r < a.runs; ++r) {
+        const int start = table.get(0, r), end = table.get(1, r), rank = table.get(2, r), first = table.get(3, r);
+        const float scale = __uint_as_float(uint32_t(__builtin_amdgcn_readlane(int(__float_as_uint(table.scale)), r)));
+        const bool mine = t0 + tok >= start && t0 + tok < end, lost = (bad >> r) & 1;
+#pragma unroll
+        for (int f = 0; f < C::FB; ++f) {
+            const int j = (wave / 2 * C::FB + f) * 16 + 4 * quad;
+            const bool in = mine && j >= first && j < first + rank;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[f][i] = in ? (lost ? __uint_as_float(0x7fc00000u) : acc[f][0][i] * scale) : v[f][i];
+        }
+    }
+#pragma unroll
+    for (int f = 0; f < C::FB; ++f) {
+        const int j = (wave / 2 * C::FB + f) * 16 + 4 * quad;
+        const bf16x4 hi = __builtin_convertvector(v[f], bf16x4), lo = __builtin_convertvector(v[f] - __builtin_convertvector(hi, f32x4), bf16x4);
+        const uint32_t to = few + kFewT + j / kRanks * 4096 + tok * 64 + j % kRanks * 2;
+        lds_store<bf16x4>(to, hi);
+        lds_store<bf16x4>(to + 2048, lo);
+    }
+    __syncthreads();
+}
+
+template <typename C, typename Args>
+__device__ __forceinline__ void few_up(uint32_t few, const Args &a, int wave, int lane, f32x4 (&acc)[C::FB][C::TB]) {
+    const int col = lane % 16, quad = lane / 16;
+#pragma unroll
+    for (int e = 0; e < kFewRanks / kRanks; ++e) {
+        if (e * kRanks >= a.ranks) break;
+        const uint32_t t_at = few + kFewT + e * 4096 + (wave % 2 * 16 + col) * 64 + 16 * quad;
+        const bf16x8 hi = lds_load<bf16x8>(t_at), lo = lds_load<bf16x8>(t_at + 2048);
+#pragma unroll
+        for (int f = 0; f < C::FB; ++f) {
+            const bf16x8 u = lds_load<bf16x8>(few + kFewU + e * 4096 + ((wave / 2 * C::FB + f) * 16 + col) * 64 + 16 * quad);
+            acc[f][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u, hi, acc[f][0], 0, 0, 0);
+            acc[f][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u, lo, acc[f][0], 0, 0, 0);
+        }
+    }
+}
+
 // Coordinates of token tk in its request's grid; the lanes' tokens lie between `first` and `last`, mostly of one request.
 __device__ __forceinline__ void grid_position(const AdaptedArgs<true> &a, int32_t tk, int32_t first, int32_t last, float &t, float &h, float &w) {
     const int lane = threadIdx.x % 64;
@@ -803,7 +960,7 @@ __device__ __forceinline__ void norm_rope(f32x4 (&acc)[C::FB][C::TB], F &&sum_sq
 #pragma unroll
     for (int t = 0; t < C::TB; ++t) {
         const uint32_t tk = uint32_t(min(tok_first + 16 * t + col, a.n - 1));
-        if constexpr (kAdapted<Args>) {
+        if constexpr (kGrids<Args>) {
             grid_position(a, int32_t(tk), min(tok_first + 16 * t, a.n - 1), min(tok_first + 16 * t + 15, a.n - 1), pt[t], ph[t], pw[t]);
         } else {
             const uint32_t ct = fastdiv(tk, r.hw), rem = tk - ct * r.hw.d, ch = fastdiv(rem, r.w);
@@ -890,9 +1047,18 @@ __device__ __forceinline__ void run_tile(uint32_t lds0, const Args &a, int f0, i
         turns_pre = f32x4{tp[0], tp[1], tp[2], 0.0f};
     }
     f32x4 acc[FB][TB];
+    auto few_table = [&] {
+        if constexpr (kFew<Args>) return FewTable(a.few, lane);
+        else return 0;
+    }();
     if constexpr (C::SPLIT) product_split_k<C>(lds0, a, f0, t0, wave, lane, acc, table);
     else if constexpr (C::HOW == kWide) product_wide<C>(lds0, a, f0, t0, wave, lane, acc, table);
     else product<C>(lds0, a, f0, t0, wave, lane, acc, table);
+    if constexpr (kFew<Args>) {
+        stage_barrier<0>();                              // the stages are free
+        few_down<C>(lds0, table, a, few_table, f0, t0, wave, lane);
+        few_up<C>(table, a, wave, lane, acc);
+    }
 
     stage_barrier<0>();                                  // the ring is free: every wave has read its last operand
     const uint32_t out_lds = lds0 + wave * (16 * FB * 32), rope_lds = lds0 + C::kOut, ss_lds = rope_lds + kMaxPairs * 16;
@@ -1003,8 +1169,7 @@ __global__ __launch_bounds__(P::kThreads, P::HOW == kShared ? 2 : 1) void gemm_k
     }
 }
 
-// Fills the device-side rotary description; LP_OK or the error.
-int make_rope_args(const lp_rope *rope, int64_t n, int32_t head_dim, float eps, RopeArgs *out) {
+int check_rope(const lp_rope *rope, int64_t n, int32_t head_dim, float eps) {
     if (rope == nullptr) return LP_ERR_INVALID_ARG;
     int64_t cells = 1;
     int32_t sum = 0;
@@ -1014,7 +1179,13 @@ int make_rope_args(const lp_rope *rope, int64_t n, int32_t head_dim, float eps, 
         sum += rope->split[ax];
     }
     if (cells != n || sum != head_dim || !(rope->base > 0.0f) || !(eps >= 0.0f)) return LP_ERR_INVALID_ARG;
-    if (n >= (int64_t(1) << 31)) return LP_ERR_UNSUPPORTED;
+    return n >= (int64_t(1) << 31) ? LP_ERR_UNSUPPORTED : LP_OK;
+}
+
+// Fills the device-side rotary description; LP_OK or the error.
+int make_rope_args(const lp_rope *rope, int64_t n, int32_t head_dim, float eps, RopeArgs *out) {
+    const int rc = check_rope(rope, n, head_dim, eps);
+    if (rc != LP_OK) return rc;
     RopeArgs r{};
     int pair = 0;
     for (int ax = 0; ax < 3; ++ax) {
@@ -1130,7 +1301,7 @@ Plan pick_plan(int64_t n, int32_t d_in, int32_t d_out, bool small_ok, int cus) {
 
 template <bool QKV, int HD, typename P, typename R, typename Args>
 int launch_tiles(Args a, int64_t whole, hipStream_t stream) {
-    constexpr int kLds = (P::kLds > R::kLds ? P::kLds : R::kLds) + (kAdapted<Args> ? kTableBytes : 0);
+    constexpr int kLds = (P::kLds > R::kLds ? P::kLds : R::kLds) + (kAdapted<Args> ? kTableBytes : kFew<Args> ? kFewBytes : 0);
     static_assert(kLds <= 160 * 1024, "the LDS of a compute unit");
     static std::atomic<uint64_t> attr_set{0};
     const void *kern = reinterpret_cast<const void *>(&gemm_kernel<QKV, HD, P, R, Args>);

@@ -22,7 +22,7 @@ EPS = 1e-6
 
 
 def way(lengths, ranks, d_in, d_out, head_dim=0, cus=None):
-    """What a call runs: routes.GemmWay, and the tile of the down products."""
+    """What a call runs: routes.GemmWay, and the tile of the down products ((0, 0): one launch for all)."""
     fn = lp._lib().lp_internal_adapted_way
     fn.argtypes = [C.POINTER(C.c_int64), C.POINTER(C.c_int32), C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int64)]
     starts = np.concatenate([[0], np.cumsum(lengths)]).tolist()
@@ -152,6 +152,47 @@ def test_down_products_of_every_tile(lengths, ranks, tile, d_in):
     rows = torch.tensor(sorted(set(list(range(0, c.n, max(1, c.n // 700))) + [s + i for s in c.starts for i in range(-3, 3) if 0 <= s + i < c.n])), device="cuda")
     inside(y[rows], *c.want(rows))
     assert torch.isfinite(y.float()).all()
+
+
+# one token to eight token tiles, ranks of one group of 8 rows to all eight, runs that share a tile, have none of its rows or no rows at all, fewer
+# and more k-tiles than stages
+@pytest.mark.parametrize("lengths,ranks", [
+    ([1], [8]), ([1], [64]), ([1, 1, 1, 1, 1, 1, 1, 1], [8] * 8), ([3, 0, 1, 40, 2], [16, 8, 0, 24, 8]), ([31, 1, 33], [40, 0, 24]),
+    ([200, 56], [32, 32]), ([70, 60, 50], [8, 48, 0]),
+])
+@pytest.mark.parametrize("d_in,d_out", [(64, 128), (192, 640), (576, 384), (1088, 256), (2112, 1536)])
+def test_few_rows_in_one_launch(lengths, ranks, d_in, d_out):
+    assert way(lengths, ranks, d_in, d_out)[1] == (0, 0)
+    c = Case(lengths, ranks, d_in, d_out, bias=d_in != 192, seed=21)
+    inside(c.linear(), *c.want(), (lengths, ranks))
+    c = Case(lengths, ranks, d_in, d_out, bias=False, seed=22, up=10.0)
+    c.w.zero_()
+    inside(c.linear(), *c.want(), (lengths, ranks))
+
+
+@pytest.mark.parametrize("heads,grids,ranks", [
+    (2, [(1, 1, 1)], [8]), (4, [(5, 8, 5), (1, 1, 1), (3, 5, 7)], [8, 0, 16]), (8, [(2, 3, 5), (0, 1, 1), (1, 7, 3)], [24, 8, 32]), (20, [(1, 2, 9)], [64]),
+])
+def test_qkv_of_few_rows_in_one_launch(heads, grids, ranks):
+    c = Qkv(grids, ranks, heads, 64, seed=23)
+    assert way(c.lengths, ranks, c.d_in, c.d_out, 64)[1] == (0, 0)
+    c.check()
+
+
+@pytest.mark.parametrize("where", ["x", "down", "up"])
+def test_few_rows_with_a_request_of_nan(where):
+    import torch
+    c = Case([7, 9, 20], [16, 24, 16], 320, 384)
+    assert way(c.lengths, c.ranks, 320, 384)[1] == (0, 0)
+    if where == "x":
+        c.x[8, 3], c.x[15, 319] = float("nan"), float("inf")
+    else:
+        c.adapters[1][0 if where == "down" else 1].view(-1)[-1] = float("inf")
+    y = c.linear()
+    for rows in (slice(0, 7), slice(16, 36)):
+        inside(y[rows], *c.want(rows))
+    if where == "up":
+        assert torch.isnan(y[7:16, -1].float()).all()
 
 
 def test_large_adapters_beside_small_weights():
@@ -285,7 +326,7 @@ def test_qkv_adapters_of_every_tiling(heads, hd, grid, tiles):
     import torch
     t = grid[0]
     grids = [(a,) + grid[1:] for a in (t - t // 2 - t // 3, t // 3, t // 2)]
-    c = Qkv(grids, [32, 0, 16], heads, hd)
+    c = Qkv(grids, [32, 0, 40], heads, hd)
     assert str(way(c.lengths, c.ranks, c.d_in, c.d_out, hd)[0]) == tiles
     edges = [s + i for s in c.starts for i in (-2, -1, 0, 1) if 0 <= s + i < c.n]
     c.check(torch.tensor(sorted(set(edges + list(range(0, c.n, max(1, c.n // 150))))), device="cuda"))
