@@ -408,6 +408,9 @@ def make_norm(kind: int, eps: float, weight=None, bias=None) -> lp_norm:
 def make_modulation(gate=None, scale=None, shift=None, stride: Optional[int] = None) -> lp_modulation:
     """Vectors per request, device, binary32, which the caller keeps.  stride defaults to the row stride that the tensors
     given have in common; a vector (one dimension) is that of every request."""
+    for t in (gate, scale, shift):
+        if t is not None and not isinstance(t, int) and t.stride(-1) != 1:
+            raise ValueError("a request's vector has to be contiguous")
     if stride is None:
         strides = {int(t.stride(0)) if t.dim() > 1 else 0 for t in (gate, scale, shift) if t is not None}
         if len(strides) > 1:

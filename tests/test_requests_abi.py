@@ -69,6 +69,8 @@ def test_modulation_of_tensors_takes_their_stride():
     assert lp.make_modulation(scale=t[0, 0]).stride == 0 and lp.make_modulation().stride == 0
     with pytest.raises(ValueError):
         lp.make_modulation(scale=t[:, 0], shift=t[0, 1])
+    with pytest.raises(ValueError):
+        lp.make_modulation(scale=t[:, 0].t())
 
 
 def _adapters(*specs):
