@@ -3,13 +3,13 @@
 //   lp_linear_adapters           y = x W^T + b + s_r (x D_r^T) U_r^T
 //   lp_qkv_projection_adapters   the same in the sections q | k | v, q and k normalised and rotated
 //
-// with r the request that a row belongs to.  Two launches (one for few rows, few_down of lp_gemm.h): adapter_down_kernel forms t = s_r x D_r^T of the rows that have an
+// with r the request that a row belongs to.  Two launches (one for few rows, product_few of lp_gemm.h): adapter_down_kernel forms t = s_r x D_r^T of the rows that have an
 // adapter (and looks over every U_r), and the product of lp_gemm.h takes t and U_r as further k-tiles.  The second thus costs a k-tile of 64 for every
 // 32 ranks beside d_in / 64 of them, and no pass over y.
 //
 // What bounds it.  Large calls: the shared product; 24570 x 5120 -> 5120 with ranks 64 and 16 966 us, 900 without adapters, 64 of the
 // difference for t, which reads x once more (3.9 TB/s).  q | k | v of 13230 x 5120, rank 32, 1557 and 1506, 41 for t.  Few rows and ranks: one
-// launch (few_down); with more ranks two, 6 rows of d_in 1536 and rank 128 13.3 us, 5.4 without adapters.
+// launch (product_few); with more ranks two, 6 rows of d_in 1536 and rank 128 13.3 us, 5.4 without adapters.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -223,7 +223,7 @@ int run_down(DownArgs &d, int32_t runs, int dev, int cus, hipStream_t stream) {
     }
 }
 
-// Whether a call is taken in one launch (few_down): one round of 64 x 32 tiles at most, and ranks for one product of 64 rows.
+// Whether a call is taken in one launch (product_few): one round of 64 x 32 tiles at most, and ranks for one product of 64 rows.
 bool takes_few(int64_t n, int32_t d_out, int32_t head_dim, int cus, int32_t runs, const DownRun *run) {
     if (!small_tilings(head_dim) || (n + Split64x32::kT - 1) / Split64x32::kT * ((d_out + Split64x32::kF - 1) / Split64x32::kF) > cus) return false;
     int ranks = 0;

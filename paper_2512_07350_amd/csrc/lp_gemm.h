@@ -98,7 +98,7 @@ struct AdaptedArgs<true> : AdaptedArgs<false> {
     int32_t requests;
     RequestGrid grid[LP_MAX_REQUESTS];
 };
-// Few rows and few ranks: the whole in one launch, see few_down.
+// Few rows and few ranks: the whole in one launch, see product_few.
 constexpr int kFewRuns = 8, kFewRanks = 64;
 struct FewRun {
     const __bf16 *down, *up;
@@ -118,7 +118,7 @@ template <typename Args>
 constexpr bool kAdapted = std::is_base_of<AdaptedArgs<false>, Args>::value && !kFew<Args>;       // takes adapters as k-tiles
 template <typename Args>
 constexpr bool kGrids = std::is_base_of<AdaptedArgs<true>, Args>::value;                         // every request has its grid
-// A product whose W is made of groups of 8 rows that lie anywhere: those that a wavefront loads (product_split_k)
+// A product of 64 rows of W and 64 more, groups of 8 that lie anywhere: those that a wavefront loads (product_split_k)
 struct GroupedArgs : GemmHead {
     __amdgpu_buffer_rsrc_t group[2];
 };
@@ -687,10 +687,10 @@ __device__ __forceinline__ void product_split_k(uint32_t lds0, const Args &a, in
         const bool is_x = i < C::kLoadsX;
         const int rows8 = wave + (is_x ? i : i - C::kLoadsX) * W;
         if constexpr (std::is_same<Args, GroupedArgs>::value) {
-            static_assert(C::kF == 16 * W, "two groups to a wave");
-            if (!is_x) {
-                load_to_lds_16(a.group[i - C::kLoadsX], __builtin_amdgcn_readfirstlane(lds0 + stage + rows8 * 1024), kt < n_plain ? voff : 0x80000000u,
-                               __builtin_amdgcn_readfirstlane(uint32_t(kt) * kRowBytes));
+            static_assert(C::kF == 128 && W == 4, "two groups to a wave behind two of W");
+            if (i >= C::kLoadsX + 2) {
+                load_to_lds_16(a.group[i - C::kLoadsX - 2], __builtin_amdgcn_readfirstlane(lds0 + stage + rows8 * 1024),
+                               kt < n_plain ? voff : 0x80000000u, __builtin_amdgcn_readfirstlane(uint32_t(kt) * kRowBytes));
                 return;
             }
         }
@@ -789,28 +789,33 @@ __device__ __forceinline__ void product_split_k(uint32_t lds0, const Args &a, in
 #pragma unroll
         for (int t = 0; t < TB; ++t) *LP_LDS_PTR(f32x4, uintptr_t(lds0 + ((wave * FB + f) * TB + t) * 1024 + 16 * lane)) = part[f][t];
     __syncthreads();
-    const int f_own = (wave / C::WT) * C::FB, t_own = (wave % C::WT) * C::TB;
+    // with groups a wave has two blocks of W and two, four further on, of the others
+    constexpr bool kGrouped = std::is_same<Args, GroupedArgs>::value;
+    const int f_own = (wave / C::WT) * (kGrouped ? 2 : C::FB), t_own = (wave % C::WT) * C::TB;
 #pragma unroll
     for (int f = 0; f < C::FB; ++f)
 #pragma unroll
         for (int t = 0; t < C::TB; ++t) {
-            f32x4 sum = lds_load<f32x4>(lds0 + ((f_own + f) * TB + t_own + t) * 1024 + 16 * lane);
+            const int b = kGrouped ? f / 2 * 4 + f % 2 : f;
+            f32x4 sum = lds_load<f32x4>(lds0 + ((f_own + b) * TB + t_own + t) * 1024 + 16 * lane);
 #pragma unroll
-            for (int w = 1; w < W; ++w) sum += lds_load<f32x4>(lds0 + ((w * FB + f_own + f) * TB + t_own + t) * 1024 + 16 * lane);
+            for (int w = 1; w < W; ++w) sum += lds_load<f32x4>(lds0 + ((w * FB + f_own + b) * TB + t_own + t) * 1024 + 16 * lane);
             acc[f][t] = sum;
         }
 }
 
 // Calls of few rows in one launch.  Every workgroup of 64 features x 32 tokens forms t of its tokens itself, for the ranks of all runs one after
-// the other (at most 64, so that one more product of 64 rows does: those of the D's, a group of 8 rows to a load), and adds
-//   sum_j U[feature, j] (hi + lo)[token, j]
-// to its product.  t is zero where the token is not of j's run.  It costs the k-tiles of x a second time, in every workgroup, and saves the launch
-// in front and the trip through memory.
+// the other (at most 64): its product has 64 rows more, those of the D's, a group of 8 to a load; then
+//   y += sum_j U[feature, j] (hi + lo)[token, j],
+// t being zero where the token is not of j's run.  It costs D in every workgroup, and saves the launch in front and the trip through memory:
+// 6 rows of d_in 1536 in two launches 12.5 us, with the two products one after the other 10.1, as one 9.6 (eight stages 9.9; without adapters 5.4); q | k | v
+// of 306 x 256 10.5, 8.5, 7.9.
 //
-// LDS at `few`: t as kFewRanks / 32 times hi and lo, 32 tokens of 32 ranks; U as 64 features of 32 ranks; the runs whose U is not finite.
-constexpr int kFewT = 0, kFewU = 8192, kFewBad = 16384, kFewBytes = 16384 + 64;
+// LDS behind the stages: t as kFewRanks / 32 times hi and lo, 32 tokens of 32 ranks; U as 64 features of 32 ranks; the runs whose U is not finite.
+using FewTile = Tiling<2, 2, 4, 1, 6, kSplitK>;          // of W's 64 features and the D's 64 rows
+constexpr int kFewU = 8192, kFewBad = 16384, kFewBytes = 16384 + 64;
 
-// The runs, one to a lane (the first kFewRuns): fetched in front of the product and looked at behind it, where they have long arrived.
+// The runs, one to a lane (the first kFewRuns).
 struct FewTable {
     u32x4 where;                         // down, up
     u32x4 rows;                          // start, end, rank, first
@@ -828,13 +833,17 @@ struct FewTable {
     }
 };
 
+// Leaves a wave's blocks of the tile C (64 x 32) in acc, like product_split_k.
 template <typename C, typename Args>
-__device__ __forceinline__ void few_down(uint32_t lds0, uint32_t few, const Args &a, const FewTable &table, int f0, int t0, int wave, int lane) {
-    static_assert(C::SPLIT && C::kF == 64 && C::kT == 32 && C::kWaves == 4, "the layouts here");
+__device__ __forceinline__ void product_few(uint32_t lds0, const Args &a, int f0, int t0, int wave, int lane, f32x4 (&acc)[C::FB][C::TB]) {
+    static_assert(C::SPLIT && C::kF == 64 && C::kT == 32 && C::kWaves == 4 && C::FB == 2 && C::TB == 1 && FewTile::kT == 32, "the layouts here");
     const int col = lane % 16, quad = lane / 16, tid = threadIdx.x;
     const int section = kGrids<Args> ? f0 / (a.d_out / 3) : 0;
+    const uint32_t few = lds0 + FewTile::kLds;
+    const FewTable table(a.few, lane);
     GroupedArgs g{};
-    g.x = g.w = a.x;                                     // in w's place: the groups
+    g.x = a.x;
+    g.w = a.w;
     g.n = a.n;
     g.d_in = a.d_in;
     g.d_out = a.d_out;
@@ -866,8 +875,10 @@ __device__ __forceinline__ void few_down(uint32_t lds0, uint32_t few, const Args
     if (from_u != nullptr)
 #pragma unroll
         for (int h = 0; h < 2; ++h) piece[h] = *reinterpret_cast<const u32x4 *>(from_u + int64_t(f0 + tid / 8 + 32 * h) * u_rank);
-    f32x4 acc[C::FB][C::TB];
-    product_split_k<C>(lds0, g, 0, t0, wave, lane, acc, 0);
+    f32x4 both[FewTile::FB][FewTile::TB];                // two blocks of W x, two of D x
+    product_split_k<FewTile>(lds0, g, f0, t0, wave, lane, both, 0);
+#pragma unroll
+    for (int f = 0; f < C::FB; ++f) acc[f][0] = both[f][0];
     uint32_t bad = 0;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -887,41 +898,36 @@ __device__ __forceinline__ void few_down(uint32_t lds0, uint32_t few, const Args
         lds_store<u32x4>(few + kFewU + j_piece / kRanks * 4096 + (tid / 8 + 32 * h) * 64 + j_piece % kRanks * 2, piece[h]);
     }
     const int tok = wave % 2 * 16 + col;
-    f32x4 v[C::FB] = {};
+    f32x4 v[2] = {};
     for (int r = 0; r < a.runs; ++r) {
         const int start = table.get(0, r), end = table.get(1, r), rank = table.get(2, r), first = table.get(3, r);
         const float scale = __uint_as_float(uint32_t(__builtin_amdgcn_readlane(int(__float_as_uint(table.scale)), r)));
         const bool mine = t0 + tok >= start && t0 + tok < end, lost = (bad >> r) & 1;
 #pragma unroll
-        for (int f = 0; f < C::FB; ++f) {
-            const int j = (wave / 2 * C::FB + f) * 16 + 4 * quad;
+        for (int f = 0; f < 2; ++f) {
+            const int j = (wave / 2 * 2 + f) * 16 + 4 * quad;
             const bool in = mine && j >= first && j < first + rank;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[f][i] = in ? (lost ? __uint_as_float(0x7fc00000u) : acc[f][0][i] * scale) : v[f][i];
+            for (int i = 0; i < 4; ++i) v[f][i] = in ? (lost ? __uint_as_float(0x7fc00000u) : both[2 + f][0][i] * scale) : v[f][i];
         }
     }
 #pragma unroll
-    for (int f = 0; f < C::FB; ++f) {
-        const int j = (wave / 2 * C::FB + f) * 16 + 4 * quad;
+    for (int f = 0; f < 2; ++f) {
+        const int j = (wave / 2 * 2 + f) * 16 + 4 * quad;
         const bf16x4 hi = __builtin_convertvector(v[f], bf16x4), lo = __builtin_convertvector(v[f] - __builtin_convertvector(hi, f32x4), bf16x4);
-        const uint32_t to = few + kFewT + j / kRanks * 4096 + tok * 64 + j % kRanks * 2;
+        const uint32_t to = few + j / kRanks * 4096 + tok * 64 + j % kRanks * 2;
         lds_store<bf16x4>(to, hi);
         lds_store<bf16x4>(to + 2048, lo);
     }
     __syncthreads();
-}
-
-template <typename C, typename Args>
-__device__ __forceinline__ void few_up(uint32_t few, const Args &a, int wave, int lane, f32x4 (&acc)[C::FB][C::TB]) {
-    const int col = lane % 16, quad = lane / 16;
 #pragma unroll
     for (int e = 0; e < kFewRanks / kRanks; ++e) {
         if (e * kRanks >= a.ranks) break;
-        const uint32_t t_at = few + kFewT + e * 4096 + (wave % 2 * 16 + col) * 64 + 16 * quad;
+        const uint32_t t_at = few + e * 4096 + tok * 64 + 16 * quad;
         const bf16x8 hi = lds_load<bf16x8>(t_at), lo = lds_load<bf16x8>(t_at + 2048);
 #pragma unroll
-        for (int f = 0; f < C::FB; ++f) {
-            const bf16x8 u = lds_load<bf16x8>(few + kFewU + e * 4096 + ((wave / 2 * C::FB + f) * 16 + col) * 64 + 16 * quad);
+        for (int f = 0; f < 2; ++f) {
+            const bf16x8 u = lds_load<bf16x8>(few + kFewU + e * 4096 + ((wave / 2 * 2 + f) * 16 + col) * 64 + 16 * quad);
             acc[f][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u, hi, acc[f][0], 0, 0, 0);
             acc[f][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u, lo, acc[f][0], 0, 0, 0);
         }
@@ -1047,18 +1053,10 @@ __device__ __forceinline__ void run_tile(uint32_t lds0, const Args &a, int f0, i
         turns_pre = f32x4{tp[0], tp[1], tp[2], 0.0f};
     }
     f32x4 acc[FB][TB];
-    auto few_table = [&] {
-        if constexpr (kFew<Args>) return FewTable(a.few, lane);
-        else return 0;
-    }();
-    if constexpr (C::SPLIT) product_split_k<C>(lds0, a, f0, t0, wave, lane, acc, table);
+    if constexpr (kFew<Args>) product_few<C>(lds0, a, f0, t0, wave, lane, acc);
+    else if constexpr (C::SPLIT) product_split_k<C>(lds0, a, f0, t0, wave, lane, acc, table);
     else if constexpr (C::HOW == kWide) product_wide<C>(lds0, a, f0, t0, wave, lane, acc, table);
     else product<C>(lds0, a, f0, t0, wave, lane, acc, table);
-    if constexpr (kFew<Args>) {
-        stage_barrier<0>();                              // the stages are free
-        few_down<C>(lds0, table, a, few_table, f0, t0, wave, lane);
-        few_up<C>(table, a, wave, lane, acc);
-    }
 
     stage_barrier<0>();                                  // the ring is free: every wave has read its last operand
     const uint32_t out_lds = lds0 + wave * (16 * FB * 32), rope_lds = lds0 + C::kOut, ss_lds = rope_lds + kMaxPairs * 16;
@@ -1301,7 +1299,7 @@ Plan pick_plan(int64_t n, int32_t d_in, int32_t d_out, bool small_ok, int cus) {
 
 template <bool QKV, int HD, typename P, typename R, typename Args>
 int launch_tiles(Args a, int64_t whole, hipStream_t stream) {
-    constexpr int kLds = (P::kLds > R::kLds ? P::kLds : R::kLds) + (kAdapted<Args> ? kTableBytes : kFew<Args> ? kFewBytes : 0);
+    constexpr int kLds = kFew<Args> ? FewTile::kLds + kFewBytes : (P::kLds > R::kLds ? P::kLds : R::kLds) + (kAdapted<Args> ? kTableBytes : 0);
     static_assert(kLds <= 160 * 1024, "the LDS of a compute unit");
     static std::atomic<uint64_t> attr_set{0};
     const void *kern = reinterpret_cast<const void *>(&gemm_kernel<QKV, HD, P, R, Args>);
