@@ -195,6 +195,15 @@ def test_few_rows_with_a_request_of_nan(where):
         assert torch.isnan(y[7:16, -1].float()).all()
 
 
+def test_more_elements_than_32_bits_count():
+    """x of 2.2e9 elements; rows at its ends, at the border of the requests and behind element 2^31."""
+    import torch
+    c = Case([200000, 160001], [16, 32], 6144, 128)
+    y = c.linear()
+    rows = torch.tensor([0, 1, 199999, 200000, 349524, 349525, 349526, 349530, 359999, 360000], device="cuda")
+    inside(y[rows], *c.want(rows))
+
+
 def test_large_adapters_beside_small_weights():
     """The adapter's part a hundred times the projection's: t keeps 17 bits."""
     c = Case([300, 50], [64, 16], 512, 256, up=20.0)
