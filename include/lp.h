@@ -339,7 +339,10 @@ typedef struct lp_adapter {
  * An infinity or a NaN in x, in down or in up makes rows of the requests that they belong to unspecified (typically NaN); rows
  * of other requests are not affected.
  * One small launch for the down products, whose results are kept as two bf16 each (2^-17 relative), then one for
- * the rest: the adapters are further terms of w's sums, in binary32, with one rounding to bf16 on store.
+ * the rest: the adapters are further terms of w's sums, in binary32, with one rounding to bf16 on store.  With few
+ * rows and ranks one launch does both.  A call's results are the same every time; in another batch a row may differ in its last
+ * bit, where the sums are formed in another order (lp_norm_modulate and lp_gated_residual_norm give a row the same
+ * result in every batch of one alignment).
  */
 int lp_linear_adapters(const void *x, const void *w, const float *bias, void *y, const lp_requests *requests,
                        int32_t d_in, int32_t d_out, const lp_adapter *adapters, void *workspace, int64_t workspace_bytes,

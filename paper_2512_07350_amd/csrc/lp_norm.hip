@@ -360,6 +360,7 @@ extern "C" int lp_gated_residual_norm(const void *h, int32_t h_type, const void 
     if (post != nullptr && (rc = check_norm(post, &a.post, &a.post_eps, &a.post_weight, &a.post_bias)) != LP_OK) return rc;
     if (norm != nullptr && (rc = check_norm(norm, &a.norm, &a.eps, &a.weight, &a.bias)) != LP_OK) return rc;
     if ((norm == nullptr) != (y == nullptr) && a.n > 0) return LP_ERR_INVALID_ARG;
+    if (norm == nullptr) a.scale = a.shift = nullptr;
     if (a.n == 0) return LP_OK;
     const int size = h_type == LP_F32 ? 4 : 2;
     if (h == nullptr || u == nullptr || h_out == nullptr || !aligned(h, size) || !aligned(h_out, size) || !aligned(u, 2) || !aligned(y, 2))

@@ -269,3 +269,20 @@ def test_on_another_stream_and_replayed_from_a_graph():
         call(torch.cuda.current_stream().cuda_stream)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, (o, y, u)))
+
+
+def test_a_row_is_the_same_in_every_batch():
+    import torch
+    st = torch.cuda.current_stream().cuda_stream
+    for d in (776, 1153, 5120):
+        c = Case([900, 1500, 600], d, "f32", "layer", "rms")
+        req, norm, post, mod = c.host_structs()
+        (h, _), (u, _) = c.dev(c.h, "f32"), c.dev(c.u, "bf16")
+        o, y = torch.empty_like(h), torch.empty_like(u)
+        lp.lp_gated_residual_norm(h, lp.LP_F32, u, o, y, req, d, post, norm, mod, stream=st)
+        alone = slice(1700, 1703)
+        o1, y1 = torch.empty_like(h[alone]), torch.empty_like(u[alone])
+        gate, scale, shift = (torch.from_numpy(c.vec[k][1:2].copy()).cuda() for k in ("gate", "scale", "shift"))
+        lp.lp_gated_residual_norm(h[alone], lp.LP_F32, u[alone], o1, y1, lp.make_requests([0, 3]), d, post, norm, lp.make_modulation(gate, scale, shift),
+                                  stream=st)
+        assert torch.equal(o[alone], o1) and torch.equal(y[alone], y1)
