@@ -372,6 +372,39 @@ def test_two_calls_on_two_streams_with_a_workspace_each():
     assert all(torch.equal(y, w) for (y, _), w in zip(outs, want))
 
 
+def test_two_graphs_with_a_workspace_each():
+    """Calls of two launches, captured, and replayed in turn on two streams with eager calls between."""
+    import torch
+    cases, graphs, outs, tables = [Case([900, 0, 600, 40], [64, 8, 16, 0], 1536, 1536, seed=31), Case([300, 5000], [96, 24], 640, 384, seed=32)], [], [], []
+    for c in cases:
+        assert way(c.lengths, c.ranks, c.d_in, c.d_out)[1] != (0, 0)
+        y, (ws, size) = torch.empty(c.n, c.d_out, dtype=torch.bfloat16, device="cuda"), c.workspace()
+        call = lambda c=c, y=y, ws=ws, size=size: lp.lp_linear_adapters(c.x, c.w, c.bias, y, lp.make_requests(c.starts), c.d_in, c.d_out,
+                                                                       lp.make_adapters(c.adapters), ws, size, torch.cuda.current_stream().cuda_stream)
+        call()
+        torch.cuda.synchronize()
+        side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            call()
+        graphs.append((graph, side))
+        outs.append(y)
+        tables.append(ws)
+    for turn in range(4):
+        for c, y, ws in zip(cases, outs, tables):
+            c.x.mul_(0.5)
+            y.fill_(float("nan"))
+            ws.fill_(float("nan"))                         # contents are irrelevant on entry
+        torch.cuda.synchronize()
+        for graph, side in graphs:
+            with torch.cuda.stream(side):
+                graph.replay()
+        torch.cuda.synchronize()
+        for c, y in zip(cases, outs):
+            assert torch.equal(y, c.linear())              # eager, with a workspace of its own
+    for c, y in zip(cases, outs):
+        inside(y, *c.want())
+
+
 def test_the_blocks_of_two_requests_from_a_graph():
     """The self-attention half of a block over a packed batch: modulated norm, projection with adapters, attention per request, output projection with
     adapters, gated residual and the next norm.  Replayed with other inputs, and every link against its definition on what it was given."""
