@@ -223,22 +223,31 @@ int run_down(DownArgs &d, int32_t runs, int dev, int cus, hipStream_t stream) {
     }
 }
 
-// Whether a call is taken in one launch (product_few): one round of 64 x 32 tiles at most, and ranks for one product of 64 rows.
+// Whether a call is taken in one launch (product_few): one round of 64 x 32 tiles at most, and in each of them ranks for one product of 64 rows.
+// us of one launch / of two: 320 x 1536 -> 1536 10.0 / 13.9, 4000 x 4096 -> 128 17.6 / 25.8, 96 x 6144 -> 5120 26.5 / 30.3, 2000 x 256 -> 256 6.4 / 9.5; in
+// two rounds 400 x 1536 -> 1536 18.9 / 14.1, 1000 x 512 -> 1536 11.9 / 11.3, 6000 x 4096 -> 128 33.3 / 28.6.
 bool takes_few(int64_t n, int32_t d_out, int32_t head_dim, int cus, int32_t runs, const DownRun *run) {
     if (!small_tilings(head_dim) || (n + Split64x32::kT - 1) / Split64x32::kT * ((d_out + Split64x32::kF - 1) / Split64x32::kF) > cus) return false;
-    int ranks = 0;
-    for (int i = 0; i < runs; ++i) ranks += run[i].rank;
-    return ranks > 0 && ranks <= kFewRanks;              // of 8 each at least: no more than kFewRuns
+    int adapters = 0, ranks = 0, tile = -1;              // ranks in the last tile so far
+    for (int i = 0; i < runs; ++i) {
+        if (run[i].rank == 0) continue;
+        const int first = run[i].start / Split64x32::kT, last = (run[i + 1].start - 1) / Split64x32::kT;
+        ranks = run[i].rank + (first == tile ? ranks : 0);
+        if (ranks > kFewRanks) return false;
+        if (last > first) ranks = run[i].rank;
+        tile = last;
+        ++adapters;
+    }
+    return adapters > 0 && adapters <= kFewRuns;
 }
 template <bool QKV, int HD>
 int launch_few(const AdaptedArgs<QKV> &a, const DownArgs &d, int32_t runs, hipStream_t stream) {
     FewArgs<QKV> few{};
     static_cast<AdaptedArgs<QKV> &>(few) = a;
-    for (int i = 0; i < runs; ++i) {
-        if (d.run[i].rank == 0) continue;
-        few.few[few.runs++] = FewRun{d.run[i].down, d.run[i].up, d.run[i].start, d.run[i + 1].start, d.run[i].rank, few.ranks, d.run[i].scale, {0, 0, 0}};
-        few.ranks += d.run[i].rank;
-    }
+    int adapters = 0;
+    for (int i = 0; i < runs; ++i)
+        if (d.run[i].rank > 0)
+            few.few[adapters++] = FewRun{d.run[i].down, d.run[i].up, d.run[i].start, d.run[i + 1].start, d.run[i].rank, d.run[i].scale};
     const int64_t tiles = (int64_t(a.n) + Split64x32::kT - 1) / Split64x32::kT * ((a.d_out + Split64x32::kF - 1) / Split64x32::kF);
     return launch_tiles<QKV, HD, Split64x32, Split64x32>(few, tiles, stream);
 }

@@ -98,19 +98,16 @@ struct AdaptedArgs<true> : AdaptedArgs<false> {
     int32_t requests;
     RequestGrid grid[LP_MAX_REQUESTS];
 };
-// Few rows and few ranks: the whole in one launch, see product_few.
-constexpr int kFewRuns = 8, kFewRanks = 64;
-struct FewRun {
+// Few rows, and few ranks in every tile: the whole in one launch, see product_few.
+constexpr int kFewRuns = 32, kFewRanks = 64;
+struct alignas(16) FewRun {
     const __bf16 *down, *up;
     int32_t start, end, rank;
-    int32_t first;               // its place among the ranks of all runs
     float scale;
-    int32_t unused[3];
 };
 template <bool QKV>
 struct FewArgs : AdaptedArgs<QKV> {
-    int32_t runs, ranks;
-    alignas(16) FewRun few[kFewRuns];    // past the last: rank 0
+    FewRun few[kFewRuns];                // past the last: rank 0
 };
 template <typename Args>
 constexpr bool kFew = std::is_base_of<FewArgs<false>, Args>::value || std::is_base_of<FewArgs<true>, Args>::value;
@@ -804,8 +801,8 @@ __device__ __forceinline__ void product_split_k(uint32_t lds0, const Args &a, in
         }
 }
 
-// Calls of few rows in one launch.  Every workgroup of 64 features x 32 tokens forms t of its tokens itself, for the ranks of all runs one after
-// the other (at most 64): its product has 64 rows more, those of the D's, a group of 8 to a load; then
+// Calls of few rows in one launch.  Every workgroup of 64 features x 32 tokens forms t of its tokens itself, for the ranks of the runs that have rows
+// in its tile one after the other (at most 64): its product has 64 rows more, those of the D's, a group of 8 to a load; then
 //   y += sum_j U[feature, j] (hi + lo)[token, j],
 // t being zero where the token is not of j's run.  It costs D in every workgroup, and saves the launch in front and the trip through memory:
 // 6 rows of d_in 1536 in two launches 12.5 us, with the two products one after the other 10.1, as one 9.6 (eight stages 9.9; without adapters 5.4); q | k | v
@@ -815,16 +812,18 @@ __device__ __forceinline__ void product_split_k(uint32_t lds0, const Args &a, in
 using FewTile = Tiling<2, 2, 4, 1, 6, kSplitK>;          // of W's 64 features and the D's 64 rows
 constexpr int kFewU = 8192, kFewBad = 16384, kFewBytes = 16384 + 64;
 
-// The runs, one to a lane (the first kFewRuns).
+// The runs, one to a lane (and again from lane kFewRuns on).
 struct FewTable {
     u32x4 where;                         // down, up
-    u32x4 rows;                          // start, end, rank, first
-    float scale;
+    u32x4 rows;                          // start, end, rank, scale
     __device__ __forceinline__ explicit FewTable(const FewRun *few, int lane) {
-        const FewRun &run = few[lane % kFewRuns];
-        where = *reinterpret_cast<const u32x4 *>(&run.down);
-        rows = *reinterpret_cast<const u32x4 *>(&run.start);
-        scale = run.scale;
+        const u32x4 *run = reinterpret_cast<const u32x4 *>(few + lane % kFewRuns);
+        where = run[0];
+        rows = run[1];
+    }
+    // Those with an adapter and rows among `count` tokens from t0 on, lane by lane.
+    __device__ __forceinline__ uint32_t in_tile(int t0, int count) const {
+        return uint32_t(__ballot(int(rows.z) > 0 && int(rows.x) - t0 < count && int(rows.y) > t0));
     }
     __device__ __forceinline__ int get(int i, int r) const { return __builtin_amdgcn_readlane(int(rows[i]), r); }
     __device__ __forceinline__ const __bf16 *pointer(int i, int r) const {
@@ -850,22 +849,22 @@ __device__ __forceinline__ void product_few(uint32_t lds0, const Args &a, int f0
     // U: 64 features x 8 pieces of 8 ranks, two to a thread
     const int j_piece = tid % 8 * 8;
     const __bf16 *from_d[2] = {a.x, a.x}, *from_u = nullptr;
-    int bytes[2] = {0, 0}, run_of = -1, u_rank = 0;
-    for (int r = 0; r < a.runs; ++r) {
-        const int start = table.get(0, r), end = table.get(1, r), rank = table.get(2, r), first = table.get(3, r);
+    int bytes[2] = {0, 0}, bit_of = 0, u_rank = 0, ranks = 0;
+    const uint32_t runs = table.in_tile(t0, C::kT);
+    for (uint32_t left = runs; left != 0; left &= left - 1) {
+        const int r = __builtin_ctz(left), rank = table.get(2, r), first = ranks;
+        ranks += rank;
         if (j_piece >= first && j_piece < first + rank) {
-            run_of = r;
+            bit_of = int(1u << r);
             u_rank = rank;
             from_u = table.pointer(1, r) + (j_piece - first);
         }
-        if (start < t0 + C::kT && end > t0) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int j = 8 * (wave + 4 * i);
-                if (j >= first && j < first + rank) {
-                    from_d[i] = table.pointer(0, r) + int64_t(section * rank + j - first) * a.d_in;
-                    bytes[i] = 16 * a.d_in;
-                }
+        for (int i = 0; i < 2; ++i) {
+            const int j = 8 * (wave + 4 * i);
+            if (j >= first && j < first + rank) {
+                from_d[i] = table.pointer(0, r) + int64_t(section * rank + j - first) * a.d_in;
+                bytes[i] = 16 * a.d_in;
             }
         }
     }
@@ -879,37 +878,38 @@ __device__ __forceinline__ void product_few(uint32_t lds0, const Args &a, int f0
     product_split_k<FewTile>(lds0, g, f0, t0, wave, lane, both, 0);
 #pragma unroll
     for (int f = 0; f < C::FB; ++f) acc[f][0] = both[f][0];
-    uint32_t bad = 0;
+    int bad = 0;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if ((piece[h][i] & 0x7f80u) == 0x7f80u || (piece[h][i] & 0x7f800000u) == 0x7f800000u) bad = 1u << run_of;
-    // of the wave: a lane's run is one of eight, so that a vote for each does
-    uint32_t words = 0;
-    for (int r = 0; r < a.runs; ++r) words |= __ballot(bad == 1u << r) != 0 ? 1u << r : 0u;
+            if ((piece[h][i] & 0x7f80u) == 0x7f80u || (piece[h][i] & 0x7f800000u) == 0x7f800000u) bad = bit_of;
+    uint32_t words = 0;                                  // of the wave
+    for (uint32_t left = runs; left != 0; left &= left - 1) words |= __ballot(bad == int(left & -left)) != 0 ? left & -left : 0u;
     if (lane == 0) lds_store<uint32_t>(few + kFewBad + 4 * wave, words);
     __syncthreads();
     const u32x4 all = lds_load<u32x4>(few + kFewBad);
-    bad = __builtin_amdgcn_readfirstlane(all.x | all.y | all.z | all.w);
+    const uint32_t lost = __builtin_amdgcn_readfirstlane(all.x | all.y | all.z | all.w);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        if (run_of >= 0 && ((bad >> run_of) & 1)) piece[h] = u32x4{0, 0, 0, 0};
+        if ((lost & uint32_t(bit_of)) != 0) piece[h] = u32x4{0, 0, 0, 0};
         lds_store<u32x4>(few + kFewU + j_piece / kRanks * 4096 + (tid / 8 + 32 * h) * 64 + j_piece % kRanks * 2, piece[h]);
     }
     const int tok = wave % 2 * 16 + col;
     f32x4 v[2] = {};
-    for (int r = 0; r < a.runs; ++r) {
-        const int start = table.get(0, r), end = table.get(1, r), rank = table.get(2, r), first = table.get(3, r);
-        const float scale = __uint_as_float(uint32_t(__builtin_amdgcn_readlane(int(__float_as_uint(table.scale)), r)));
-        const bool mine = t0 + tok >= start && t0 + tok < end, lost = (bad >> r) & 1;
+    int first = 0;
+    for (uint32_t left = runs; left != 0; left &= left - 1) {
+        const int r = __builtin_ctz(left), rank = table.get(2, r);
+        const float scale = __uint_as_float(uint32_t(table.get(3, r)));
+        const bool mine = t0 + tok >= table.get(0, r) && t0 + tok < table.get(1, r);
 #pragma unroll
         for (int f = 0; f < 2; ++f) {
             const int j = (wave / 2 * 2 + f) * 16 + 4 * quad;
             const bool in = mine && j >= first && j < first + rank;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[f][i] = in ? (lost ? __uint_as_float(0x7fc00000u) : both[2 + f][0][i] * scale) : v[f][i];
+            for (int i = 0; i < 4; ++i) v[f][i] = in ? ((lost >> r) & 1 ? __uint_as_float(0x7fc00000u) : both[2 + f][0][i] * scale) : v[f][i];
         }
+        first += rank;
     }
 #pragma unroll
     for (int f = 0; f < 2; ++f) {
@@ -922,7 +922,7 @@ __device__ __forceinline__ void product_few(uint32_t lds0, const Args &a, int f0
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < kFewRanks / kRanks; ++e) {
-        if (e * kRanks >= a.ranks) break;
+        if (e * kRanks >= ranks) break;
         const uint32_t t_at = few + e * 4096 + tok * 64 + 16 * quad;
         const bf16x8 hi = lds_load<bf16x8>(t_at), lo = lds_load<bf16x8>(t_at + 2048);
 #pragma unroll

@@ -111,7 +111,7 @@ def test_linear_adapters(lengths, ranks, d_in, d_out):
 
 TILINGS = [
     # wavefronts that share k (3 and 9 k-tiles, fewer and more than its 8 stages, 17 and 30), 64 x 64, four wavefronts to 256 features
-    (40, 192, 640, "64x32"), (77, 576, 896, "64x32"), (33, 1088, 384, "64x32"), (95, 1920, 256, "64x32"), (150, 64, 1152, "64x64"), (200, 320, 2048, "64x64"),
+    (40, 192, 640, "64x32"), (77, 576, 896, "64x32"), (33, 1088, 384, "64x32"), (95, 1920, 256, "64x32"), (150, 64, 1152, "64x64"), (300, 320, 2048, "64x64"),
     (4033, 2112, 1536, "256x128"), (2560, 4096, 6144, "256x256"), (4097, 2112, 4224, "256x256+128x128"), (4353, 2112, 4096, "256x256+128x64"),
     (6145, 2176, 3584, "256x256+256x128"),
     (66, 64, 8448, "128x64"), (1438, 1024, 1152, "128x64"), (1345, 576, 1536, "128x128"), (75077, 64, 128, "128x128+128x64"),
@@ -125,8 +125,8 @@ def test_linear_adapters_of_every_tiling(n, d_in, d_out, tiles):
     """Four requests whose edges lie inside tiles, one in the middle without adapter."""
     lengths = [n // 3 + 5, n // 4, n // 5, 0]
     lengths[3] = n - sum(lengths)
-    ranks = [32, 0, 16, 32]
-    assert str(way(lengths, ranks, d_in, d_out)[0]) == tiles
+    ranks = [72, 0, 16, 32]                              # 72: two launches
+    assert str(way(lengths, ranks, d_in, d_out)[0]) == tiles and way(lengths, ranks, d_in, d_out)[1] != (0, 0)
     c = Case(lengths, ranks, d_in, d_out)
     y = c.linear()
     edges = [s + i for s in c.starts for i in (-2, -1, 0, 1) if 0 <= s + i < n]
@@ -159,6 +159,8 @@ def test_down_products_of_every_tile(lengths, ranks, tile, d_in):
 @pytest.mark.parametrize("lengths,ranks", [
     ([1], [8]), ([1], [64]), ([1, 1, 1, 1, 1, 1, 1, 1], [8] * 8), ([3, 0, 1, 40, 2], [16, 8, 0, 24, 8]), ([31, 1, 33], [40, 0, 24]),
     ([200, 56], [32, 32]), ([70, 60, 50], [8, 48, 0]),
+    # more ranks in all than a tile takes, up to it in one; a tile's last run the next one's first
+    ([32, 32, 32, 64], [64, 64, 56, 8]), ([40, 24, 20, 13, 31, 32], [40, 24, 40, 16, 8, 64]), ([8] * 32, [16] * 32), ([33, 63, 33, 63], [32, 32, 32, 32]),
 ])
 @pytest.mark.parametrize("d_in,d_out", [(64, 128), (192, 640), (576, 384), (1088, 256), (2112, 1536)])
 def test_few_rows_in_one_launch(lengths, ranks, d_in, d_out):
@@ -171,6 +173,7 @@ def test_few_rows_in_one_launch(lengths, ranks, d_in, d_out):
 
 
 @pytest.mark.parametrize("heads,grids,ranks", [
+    (4, [(2, 3, 5), (1, 1, 2), (4, 2, 8), (1, 5, 3), (2, 7, 7)], [48, 16, 64, 0, 64]),
     (2, [(1, 1, 1)], [8]), (4, [(5, 8, 5), (1, 1, 1), (3, 5, 7)], [8, 0, 16]), (8, [(2, 3, 5), (0, 1, 1), (1, 7, 3)], [24, 8, 32]), (20, [(1, 2, 9)], [64]),
 ])
 def test_qkv_of_few_rows_in_one_launch(heads, grids, ranks):
@@ -335,7 +338,7 @@ def test_qkv_adapters_of_every_tiling(heads, hd, grid, tiles):
     import torch
     t = grid[0]
     grids = [(a,) + grid[1:] for a in (t - t // 2 - t // 3, t // 3, t // 2)]
-    c = Qkv(grids, [32, 0, 40], heads, hd)
+    c = Qkv(grids, [72, 0, 40], heads, hd)
     assert str(way(c.lengths, c.ranks, c.d_in, c.d_out, hd)[0]) == tiles
     edges = [s + i for s in c.starts for i in (-2, -1, 0, 1) if 0 <= s + i < c.n]
     c.check(torch.tensor(sorted(set(edges + list(range(0, c.n, max(1, c.n // 150))))), device="cuda"))
