@@ -394,7 +394,9 @@ typedef struct lp_modulation {
  * (modulation included, its stride a multiple of 4) rows move in 16-byte pieces.
  * Mean and variance are binary32 sums over the row held in registers, the variance about the mean; one rounding, on
  * store.  A row that holds an infinity, a NaN or values whose squares do not fit binary32 (past 1e18 or so) comes out
- * unspecified, other rows are not affected.
+ * unspecified, other rows are not affected.  weight (1 + scale) and bias (1 + scale) are formed before a row's elements meet them: an element whose
+ * scale or shift is an infinity or a NaN is what the formula gives where norm has no bias, and unspecified in the request's rows
+ * where it has one (as its gate with post's bias, in lp_gated_residual_norm); rows of other requests are not affected.
  */
 int lp_norm_modulate(const void *x, int32_t x_type, void *y, const lp_requests *requests, int32_t d, int64_t stride_x,
                      int64_t stride_y, const lp_norm *norm, const lp_modulation *modulation, void *stream);

@@ -170,14 +170,23 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void norm_kernel(const NormArgs 
                 for (int j = 0; j < N; ++j) r.v[j] = otherwise;
             }
         };
+        // bias times factor; a bias that is not there is no term, also where the factor is infinite
+        auto product = [&](float (&out)[N], const float *bias, const Row<G, CH, VEC, float> &factor) {
+            if (bias != nullptr) {
+                w.load(bias, t, a.d);
+#pragma unroll
+                for (int j = 0; j < N; ++j) out[j] = w.v[j] * factor.v[j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; ++j) out[j] = 0.0f;
+            }
+        };
         if (a.norm != kNone) {
             fetch(s, a.scale, at, 0.0f);
             fetch(w, a.weight, 0, 1.0f);
 #pragma unroll
             for (int j = 0; j < N; ++j) { s.v[j] += 1.0f; mul[j] = w.v[j] * s.v[j]; }
-            fetch(w, a.bias, 0, 0.0f);
-#pragma unroll
-            for (int j = 0; j < N; ++j) add[j] = w.v[j] * s.v[j];
+            product(add, a.bias, s);
             fetch(s, a.shift, at, 0.0f);
 #pragma unroll
             for (int j = 0; j < N; ++j) add[j] += s.v[j];
@@ -187,9 +196,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void norm_kernel(const NormArgs 
             fetch(w, a.post_weight, 0, 1.0f);
 #pragma unroll
             for (int j = 0; j < N; ++j) gate[j] = s.v[j] * w.v[j];
-            fetch(w, a.post_bias, 0, 0.0f);
-#pragma unroll
-            for (int j = 0; j < N; ++j) gate_bias[j] = s.v[j] * w.v[j];
+            product(gate_bias, a.post_bias, s);
         }
     };
 

@@ -286,3 +286,50 @@ def test_a_row_is_the_same_in_every_batch():
         lp.lp_gated_residual_norm(h[alone], lp.LP_F32, u[alone], o1, y1, lp.make_requests([0, 3]), d, post, norm, lp.make_modulation(gate, scale, shift),
                                   stream=st)
         assert torch.equal(o[alone], o1) and torch.equal(y[alone], y1)
+
+
+@pytest.mark.parametrize("d", [264, 1153])
+@pytest.mark.parametrize("norm", ["layer", "rms"])
+@pytest.mark.parametrize("post", [None, "layer", "rms"])
+def test_infinite_vectors_where_no_bias_stands(d, norm, post):
+    """The definition has no bias there for an infinity to meet: the element is an infinity of the product's sign, and all others are as ever."""
+    import torch
+    st = torch.cuda.current_stream().cuda_stream
+    c = Case([2, 3, 2], d, "f32", norm, post)
+    c.b = c.pb = None
+    inf, rows, at = float("inf"), slice(2, 5), (0, 5, d - 1)
+    plus, minus = c.vec["scale"].copy(), c.vec["gate"].copy()
+    plus[1, at], minus[1, at] = (inf, -inf, inf), (-inf, inf, -inf)
+
+    def split(got, want, off, half, factor, what):
+        """Infinities in their places; the rest against `want`."""
+        ends = np.zeros(got.shape, bool)
+        ends[rows, at] = True
+        assert np.array_equal(got[rows][:, at], factor[rows][:, at] * np.array(what)), (got[rows][:, at], factor[rows][:, at])
+        _inside(np.where(ends, 0.0, got), np.where(ends, 0.0, want), np.where(ends, 0.0, off), half, "the rest")
+
+    # the scale
+    want, off = c.modulate(c.h.astype(np.float64), 0.0 * c.h)
+    v = _norm64(c.h.astype(np.float64), norm, c.eps, c.w, None)[0]
+    assert np.abs(v[rows][:, at]).min() > 1e-6
+    fine, c.vec["scale"] = c.vec["scale"], plus
+    req, pre, behind, mod = c.host_structs()
+    x, _ = c.dev(c.h, "f32")
+    y, _ = c.dev(None, "bf16")
+    lp.lp_norm_modulate(x, lp.LP_F32, y, req, d, pre, mod, stream=st)
+    split(y.float().cpu().numpy().astype(np.float64), want, off, HALF["bf16"], v, (inf, -inf, inf))
+    # the gate
+    c.vec["scale"] = fine
+    want, off = c.residual()
+    u = c.u.astype(np.float64)
+    u = _norm64(u, post, c.eps, c.pw, None)[0] if post else u
+    assert np.abs(u[rows][:, at]).min() > 1e-6
+    c.vec["gate"] = minus
+    req, pre, behind, mod = c.host_structs()
+    on_u, _ = c.dev(c.u, "bf16")
+    o = torch.empty_like(x)
+    lp.lp_gated_residual_norm(x, lp.LP_F32, on_u, o, y, req, d, behind, pre, mod, stream=st)
+    split(o.cpu().numpy().astype(np.float64), want, off, HALF["f32"], u, (-inf, inf, -inf))
+    others = [0, 1, 5, 6]
+    wy, oy = c.modulate(want, off)
+    _inside(y.float().cpu().numpy()[others], wy[others], oy[others], HALF["bf16"], "y")
