@@ -1169,10 +1169,10 @@ __global__ __launch_bounds__(P::kThreads, P::HOW == kShared ? 2 : 1) void gemm_k
 
 int check_rope(const lp_rope *rope, int64_t n, int32_t head_dim, float eps) {
     if (rope == nullptr) return LP_ERR_INVALID_ARG;
-    int64_t cells = 1;
-    int32_t sum = 0;
+    int64_t cells = 1, sum = 0;                          // neither passes its type, whatever the extents
     for (int ax = 0; ax < 3; ++ax) {
         if (rope->grid[ax] < 1 || rope->split[ax] < 0 || rope->split[ax] % 2 != 0) return LP_ERR_INVALID_ARG;
+        if (cells > n / rope->grid[ax]) return LP_ERR_INVALID_ARG;
         cells *= rope->grid[ax];
         sum += rope->split[ax];
     }

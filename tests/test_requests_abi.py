@@ -145,3 +145,14 @@ def test_tables_shorter_than_the_requests_are_refused():
         lp.lp_linear_adapters(1 << 20, 1 << 21, None, 1 << 22, req, 64, 128, lp.make_adapters([None]))
     with pytest.raises(ValueError):
         lp.lp_qkv_projection_adapters(1, 2, None, 3, 4, 1e-6, [lp.make_rope((1, 1, 2))], 5, 6, 7, req, 1, 128, lp.make_adapters([None] * 3))
+
+
+@pytest.mark.parametrize("grid,split", [((1, 1, 4), (2 ** 31 - 2, 2 ** 31 - 2, 68)),                 # 2^32 + 64 features
+                                        ((968973220, 49477, 384773), (64, 0, 0))])                   # 2^64 + 4 cells
+def test_rotations_that_fit_only_modulo_a_power_of_two(grid, split):
+    rope = lp.make_rope(grid, split=split, head_dim=64)
+    fine = lp.make_rope((1, 1, 6), split=split, head_dim=64)
+    assert _qkv(ropes=[rope, rope, fine]) == lp.LP_ERR_INVALID_ARG
+    assert lp._lib().lp_qkv_projection(1 << 20, 1 << 21, None, 1 << 22, 1 << 23, 1e-6, C.byref(rope), 1 << 27, 1 << 28, 1 << 29, 4, 2, 64,
+                                       None) == lp.LP_ERR_INVALID_ARG
+    assert lp._lib().lp_qk_norm_rope(1 << 20, 1 << 21, 1e-6, C.byref(rope), 4, 2, 64, 128, 64, None) == lp.LP_ERR_INVALID_ARG
