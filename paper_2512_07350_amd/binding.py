@@ -71,10 +71,12 @@ class lp_adapter(C.Structure):
 
 class lp_norm(C.Structure):
     _fields_ = [("kind", C.c_int32), ("eps", C.c_float), ("weight", C.c_void_p), ("bias", C.c_void_p)]
+    holds, given = 1 << 31, ()          # rows that its tensors suffice for, see make_norm
 
 
 class lp_modulation(C.Structure):
     _fields_ = [("gate", C.c_void_p), ("scale", C.c_void_p), ("shift", C.c_void_p), ("stride", C.c_int64)]
+    holds, vectors, given = 1 << 31, 1 << 31, ()   # see make_modulation
 
 
 class LPError(RuntimeError):
@@ -355,17 +357,44 @@ def make_requests(starts) -> lp_requests:
     return r
 
 
+def _typed(t, types, what: str) -> None:
+    """bf16 may come as its 16-bit words."""
+    if str(t.dtype) not in types:
+        raise ValueError("%s: %s, not %s" % (what, types[0], t.dtype))
+
+
+_BF16 = ("torch.bfloat16", "torch.int16", "torch.uint16")
+_F32 = ("torch.float32",)
+
+
 def make_adapters(adapters):
     """The adapters of the requests in order: (down, up, scale) with device tensors (the rank is up's second dimension) that the
     caller keeps, or None."""
     out = (lp_adapter * max(len(adapters), 1))()
+    out.given = [None] * len(adapters)      # (down's address, sections, d_in, d_out) of each
     for i, ad in enumerate(adapters):
         if ad is not None:
             down, up, scale = ad
-            if down.dim() != 2 or up.dim() != 2 or down.shape[0] % up.shape[1] or not (down.is_contiguous() and up.is_contiguous()):
+            if down.dim() != 2 or up.dim() != 2 or not (down.is_contiguous() and up.is_contiguous()):
                 raise ValueError("adapter %d: down [sections * rank, d_in] and up [d_out, rank], contiguous" % i)
-            out[i] = lp_adapter(_ptr(down), _ptr(up), int(up.shape[1]), float(scale))
+            rows, rank = int(down.shape[0]), int(up.shape[1])
+            if rows % rank if rank else rows:
+                raise ValueError("adapter %d: down [sections * rank, d_in] and up [d_out, rank], contiguous" % i)
+            _typed(down, _BF16, "adapter %d" % i)
+            _typed(up, _BF16, "adapter %d" % i)
+            out[i] = lp_adapter(_ptr(down), _ptr(up), rank, float(scale))
+            if rank:
+                out.given[i] = (out[i].down, (rows // rank, int(down.shape[1]), int(up.shape[0])))
+    sizes = {g[1] for g in out.given if g}
+    out.sizes = sizes.pop() if len(sizes) == 1 else None     # of all alike
     return out
+
+
+def _check_adapters(table, requests: lp_requests, sizes) -> None:
+    """The table of make_adapters, entries whose tensors are of another projection than sizes = (sections, d_in, d_out)."""
+    for i, g in enumerate(getattr(table, "given", ())[:requests.count if requests is not None else 0]):
+        if g and g[1] != sizes and table[i].down == g[0]:
+            raise ValueError("adapter %d: (sections, d_in, d_out) = %s for a projection of %s" % (i, g[1], sizes))
 
 
 def lp_adapter_workspace_size(n_tokens: int, rank: int, sections: int = 1) -> int:
@@ -377,15 +406,18 @@ def lp_adapter_workspace_size(n_tokens: int, rank: int, sections: int = 1) -> in
 
 def _per_request(table, requests: lp_requests, what: str):
     """A host table of structures, one for each request: the library reads as many as there are requests."""
-    if table is not None and requests is not None and len(table) < requests.count:
-        raise ValueError("%d %s for %d requests" % (len(table), what, requests.count))
+    count = len(getattr(table, "given", table)) if table is not None else 0
+    if table is not None and requests is not None and count < requests.count:
+        raise ValueError("%d %s for %d requests" % (count, what, requests.count))
     return table
 
 
 def lp_linear_adapters(x, w, bias, y, requests: lp_requests, d_in: int, d_out: int, adapters, workspace=None, workspace_bytes: int = 0,
                        stream: Optional[int] = None) -> None:
     """adapters: see make_adapters."""
-    _check(_lib().lp_linear_adapters(_ptr(x) or None, _ptr(w) or None, _ptr(bias) or None, _ptr(y) or None, _ref(requests), int(d_in), int(d_out),
+    if getattr(adapters, "sizes", None) != (1, d_in, d_out):
+        _check_adapters(adapters, requests, (1, d_in, d_out))
+    _check(_lib().lp_linear_adapters(_ptr(x) or None, _ptr(w) or None, _ptr(bias) or None, _ptr(y) or None, requests, int(d_in), int(d_out),
                                      _per_request(adapters, requests, "adapters"), _ptr(workspace) or None, int(workspace_bytes), stream or None),
            "lp_linear_adapters")
 
@@ -393,50 +425,104 @@ def lp_linear_adapters(x, w, bias, y, requests: lp_requests, d_in: int, d_out: i
 def lp_qkv_projection_adapters(x, w_qkv, bias, gain_q, gain_k, eps: float, ropes, q, k, v, requests: lp_requests, heads: int, head_dim: int,
                                adapters, workspace=None, workspace_bytes: int = 0, stream: Optional[int] = None) -> None:
     """ropes: one lp_rope (make_rope) for each request; adapters: see make_adapters."""
-    ropes = _per_request((lp_rope * max(len(ropes), 1))(*ropes), requests, "ropes")
+    ropes = (lp_rope * max(len(ropes), 1))(*_per_request(ropes, requests, "ropes"))
+    d_model = heads * head_dim
+    if getattr(adapters, "sizes", None) != (3, d_model, 3 * d_model):
+        _check_adapters(adapters, requests, (3, d_model, 3 * d_model))
     _check(_lib().lp_qkv_projection_adapters(_ptr(x) or None, _ptr(w_qkv) or None, _ptr(bias) or None, _ptr(gain_q) or None, _ptr(gain_k) or None,
-                                             float(eps), ropes, _ptr(q) or None, _ptr(k) or None, _ptr(v) or None, _ref(requests), int(heads),
+                                             float(eps), ropes, _ptr(q) or None, _ptr(k) or None, _ptr(v) or None, requests, int(heads),
                                              int(head_dim), _per_request(adapters, requests, "adapters"), _ptr(workspace) or None,
                                              int(workspace_bytes), stream or None), "lp_qkv_projection_adapters")
 
 
 def make_norm(kind: int, eps: float, weight=None, bias=None) -> lp_norm:
     """One normalisation; weight and bias are device vectors that the caller keeps."""
-    return lp_norm(int(kind), float(eps), _ptr(weight) or None, _ptr(bias) or None)
+    norm = lp_norm(int(kind), float(eps), _ptr(weight) or None, _ptr(bias) or None)
+    given = {}                              # tensor's address and elements by field
+    for name, t in (("weight", weight), ("bias", bias)):
+        if t is not None and not isinstance(t, int):
+            _typed(t, _F32, name)
+            if not t.is_contiguous():
+                raise ValueError("%s has to be contiguous" % name)
+            given[name] = (getattr(norm, name), int(t.numel()))
+    if given:
+        norm.holds, norm.given = min(n for _, n in given.values()), given
+    return norm
+
+
+def _check_norm(norm: lp_norm, d: int) -> None:
+    for name, (at, elements) in norm.given.items():
+        if at and getattr(norm, name) == at and elements < d:
+            raise ValueError("%s of %d elements for rows of %d" % (name, elements, d))
 
 
 def make_modulation(gate=None, scale=None, shift=None, stride: Optional[int] = None) -> lp_modulation:
     """Vectors per request, device, binary32, which the caller keeps.  stride defaults to the row stride that the tensors
     given have in common; a vector (one dimension) is that of every request."""
-    for t in (gate, scale, shift):
-        if t is not None and not isinstance(t, int) and t.stride(-1) != 1:
+    tensors = {k: t for k, t in (("gate", gate), ("scale", scale), ("shift", shift)) if t is not None and not isinstance(t, int)}
+    for name, t in tensors.items():
+        if t.stride(-1) != 1:
             raise ValueError("a request's vector has to be contiguous")
+        _typed(t, _F32, name)
     if stride is None:
-        strides = {int(t.stride(0)) if t.dim() > 1 else 0 for t in (gate, scale, shift) if t is not None}
+        if any(isinstance(t, int) for t in (gate, scale, shift)):
+            raise ValueError("addresses need a stride")
+        strides = {int(t.stride(0)) if t.dim() > 1 else 0 for t in tensors.values()}
         if len(strides) > 1:
             raise ValueError("gate, scale and shift need one row stride: %s" % sorted(strides))
         stride = strides.pop() if strides else 0
-    return lp_modulation(_ptr(gate) or None, _ptr(scale) or None, _ptr(shift) or None, int(stride))
+    m = lp_modulation(_ptr(gate) or None, _ptr(scale) or None, _ptr(shift) or None, int(stride))
+    given = {}                              # tensor's address, vectors, elements of one, and elements in memory by field
+    for name, t in tensors.items():
+        own = t.dim() > 1
+        vectors, elements = (int(t.shape[0]), int(t[:1].numel())) if own and m.stride else (1 << 31, int(t[:1].numel() if own else t.numel()))
+        if m.stride != (int(t.stride(0)) if own else 0):     # the caller's own stride over the tensor's memory: known with d
+            vectors = 0
+        given[name] = (getattr(m, name), vectors, elements, t.untyped_storage().nbytes() // 4 - t.storage_offset())
+    if given:
+        m.vectors, m.holds, m.given = min(g[1] for g in given.values()), min(g[2] for g in given.values()), given
+    return m
+
+
+def _check_modulation(m: lp_modulation, count: int, d: int, fields) -> None:
+    """Tensors of `fields` that do not hold a vector of d elements for every request."""
+    for name in fields:
+        at, vectors, elements, room = m.given.get(name, (None, 0, 0, 0))
+        if count > 0 and at and getattr(m, name) == at and ((count > vectors or d > elements) if vectors else (count - 1) * m.stride + d > room):
+            raise ValueError("%s does not hold %d vectors of %d elements" % (name, count, d))
 
 
 def _ref(struct):
+    """A structure by reference, or NULL."""
     return None if struct is None else C.byref(struct)
 
 
 def lp_norm_modulate(x, x_type: int, y, requests: lp_requests, d: int, norm: lp_norm, modulation: Optional[lp_modulation] = None,
                      stride_x: Optional[int] = None, stride_y: Optional[int] = None, stream: Optional[int] = None) -> None:
     """Strides default to d."""
-    _check(_lib().lp_norm_modulate(_ptr(x) or None, int(x_type), _ptr(y) or None, _ref(requests), int(d), _or(stride_x, d), _or(stride_y, d),
-                                   _ref(norm), _ref(modulation), stream or None), "lp_norm_modulate")
+    _check_vectors(requests, d, norm, None, modulation, ("scale", "shift"))
+    _check(_lib().lp_norm_modulate(_ptr(x) or None, int(x_type), _ptr(y) or None, requests, int(d), _or(stride_x, d), _or(stride_y, d),
+                                   norm, modulation, stream or None), "lp_norm_modulate")
 
 
 def lp_gated_residual_norm(h, h_type: int, u, h_out, y, requests: lp_requests, d: int, post: Optional[lp_norm], norm: Optional[lp_norm],
                            modulation: Optional[lp_modulation] = None, stride_h: Optional[int] = None, stride_u: Optional[int] = None,
                            stride_h_out: Optional[int] = None, stride_y: Optional[int] = None, stream: Optional[int] = None) -> None:
     """Strides default to d."""
-    _check(_lib().lp_gated_residual_norm(_ptr(h) or None, int(h_type), _ptr(u) or None, _ptr(h_out) or None, _ptr(y) or None, _ref(requests),
-                                         int(d), _or(stride_h, d), _or(stride_u, d), _or(stride_h_out, d), _or(stride_y, d), _ref(post),
-                                         _ref(norm), _ref(modulation), stream or None), "lp_gated_residual_norm")
+    _check_vectors(requests, d, norm, post, modulation, ("gate", "scale", "shift") if norm is not None else ("gate",))
+    _check(_lib().lp_gated_residual_norm(_ptr(h) or None, int(h_type), _ptr(u) or None, _ptr(h_out) or None, _ptr(y) or None, requests,
+                                         int(d), _or(stride_h, d), _or(stride_u, d), _or(stride_h_out, d), _or(stride_y, d), post,
+                                         norm, modulation, stream or None), "lp_gated_residual_norm")
+
+
+def _check_vectors(requests, d: int, norm, post, modulation, fields) -> None:
+    """What the tensors of make_norm and make_modulation hold, against a call: at a glance first."""
+    if norm is not None and norm.holds < d:
+        _check_norm(norm, d)
+    if post is not None and post.holds < d:
+        _check_norm(post, d)
+    if modulation is not None and requests is not None and (modulation.holds < d or modulation.vectors < requests.count):
+        _check_modulation(modulation, requests.count, d, fields)
 
 
 def _or(stride, d: int) -> int:

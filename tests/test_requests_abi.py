@@ -156,3 +156,78 @@ def test_rotations_that_fit_only_modulo_a_power_of_two(grid, split):
     assert lp._lib().lp_qkv_projection(1 << 20, 1 << 21, None, 1 << 22, 1 << 23, 1e-6, C.byref(rope), 1 << 27, 1 << 28, 1 << 29, 4, 2, 64,
                                        None) == lp.LP_ERR_INVALID_ARG
     assert lp._lib().lp_qk_norm_rope(1 << 20, 1 << 21, 1e-6, C.byref(rope), 4, 2, 64, 128, 64, None) == lp.LP_ERR_INVALID_ARG
+
+
+def _taken(call, *args, **kw):
+    """The binding hands the call on: it is the library that refuses its missing x."""
+    with pytest.raises(lp.LPError) as e:
+        call(*args, **kw)
+    assert e.value.status == lp.LP_ERR_INVALID_ARG
+
+
+def _refused(call, *args, **kw):
+    with pytest.raises(ValueError):
+        call(*args, **kw)
+
+
+def test_adapters_of_another_projection_are_refused():
+    import torch
+    z = lambda *shape, dtype=torch.bfloat16: torch.zeros(shape, dtype=dtype)
+    req, two = lp.make_requests([0, 2]), lp.make_requests([0, 2, 4])
+    linear = lambda table, r=req: lp.lp_linear_adapters(None, 1 << 21, None, 1 << 22, r, 128, 256, table, 1 << 26, 1 << 20)
+    ropes = [lp.make_rope((1, 1, 2), head_dim=64)] * 2
+    qkv = lambda table, r=req: lp.lp_qkv_projection_adapters(None, 2 << 20, None, 3 << 20, 4 << 20, 1e-6, ropes, 5 << 20, 6 << 20, 7 << 20, r, 2, 64, table,
+                                                             1 << 26, 1 << 20)
+    for_linear, for_qkv = (z(16, 128), z(256, 16), 1.0), (z(48, 128), z(384, 16), 1.0)
+    none = (z(0, 128), z(256, 0), 1.0)                     # of rank 0
+    _taken(linear, lp.make_adapters([for_linear]))
+    _taken(linear, lp.make_adapters([none, for_linear]), two)
+    _taken(linear, lp.make_adapters([for_linear, for_qkv]))                                         # the second belongs to no request
+    _taken(linear, lp.make_adapters([(z(16, 128, dtype=torch.int16), z(256, 16, dtype=torch.int16), 1.0)]))
+    _taken(qkv, lp.make_adapters([None, for_qkv]), two)
+    _refused(qkv, lp.make_adapters([for_linear]))
+    _refused(qkv, lp.make_adapters([for_qkv, for_linear]), two)
+    for down, up in (((48, 128), (256, 16)), ((16, 64), (256, 16)), ((16, 192), (256, 16)), ((16, 128), (128, 16)), ((16, 128), (384, 16))):
+        _refused(linear, lp.make_adapters([(z(*down), z(*up), 1.0)]))
+    # the table's entry is another by now: nothing is known of its sizes
+    table = lp.make_adapters([for_qkv])
+    table[0] = lp.lp_adapter(1 << 24, 1 << 25, 16, 1.0)
+    _taken(linear, table)
+    for bad in ((z(16, 128, dtype=torch.float32), z(256, 16)), (z(16, 128), z(256, 16, dtype=torch.float16)), (z(16, 128), z(256, 0)), (z(20, 128), z(256, 16))):
+        _refused(lp.make_adapters, [(*bad, 1.0)])
+    _refused(linear, lp.make_adapters([]))
+    _refused(lp.lp_qkv_projection_adapters, None, 2, None, 3, 4, 1e-6, [], 5, 6, 7, req, 2, 64, lp.make_adapters([None]))
+
+
+def test_vectors_that_do_not_hold_the_requests_are_refused():
+    import torch
+    z = lambda *shape, dtype=torch.float32: torch.zeros(shape, dtype=dtype)
+    req, pre = lp.make_requests([0, 2, 3, 3]), lp.make_norm(lp.LP_NORM_RMS, 1e-6)
+    norm = lambda mod, n=pre: lp.lp_norm_modulate(None, lp.LP_BF16, 1 << 20, req, 32, n, mod)
+    residual = lambda mod, n=pre, post=None: lp.lp_gated_residual_norm(None, lp.LP_F32, 1 << 20, 1 << 21, None if n is None else 1 << 22, req, 32, post, n, mod)
+    m = lp.make_modulation
+    all_of = z(3, 6, 32)
+    for call in (norm, residual):
+        _taken(call, m(scale=all_of[:, 1], shift=all_of[:, 5]))
+        _taken(call, m(scale=z(32)))                        # one for all
+        _taken(call, m(scale=z(1, 32).expand(2, 32)))
+        _taken(call, m(scale=z(96), stride=32))             # the caller's own stride
+        _taken(call, m(scale=z(3, 4, 8)))
+        _taken(call, m(scale=all_of.data_ptr(), stride=32))
+        _taken(call, m())
+        for bad in (m(scale=all_of[:2, 1]), m(shift=z(1, 32)), m(shift=z(3, 31)), m(scale=z(31)), m(scale=z(95), stride=32), m(shift=z(3, 32), stride=64)):
+            _refused(call, bad)
+        _refused(call, None, lp.make_norm(lp.LP_NORM_RMS, 1e-6, weight=z(31)))
+        _refused(call, None, lp.make_norm(lp.LP_NORM_LAYER, 1e-6, bias=z(8)))
+        _taken(call, None, lp.make_norm(lp.LP_NORM_LAYER, 1e-6, z(32), z(40)))
+    _refused(residual, None, pre, lp.make_norm(lp.LP_NORM_RMS, 1e-6, weight=z(31)))
+    # vectors that a call does not use
+    _taken(norm, m(gate=z(1, 32)))
+    _refused(residual, m(gate=z(1, 32)))
+    some = z(3, 64)
+    _taken(residual, m(gate=some[:, :32], scale=some[:2, :32]), None)
+    _refused(residual, m(gate=all_of[:2, 0]), None)
+    _refused(m, scale=z(3, 32, dtype=torch.bfloat16))
+    _refused(m, gate=1 << 20)
+    _refused(lp.make_norm, lp.LP_NORM_RMS, 1e-6, z(32, dtype=torch.float64))
+    _refused(lp.make_norm, lp.LP_NORM_RMS, 1e-6, z(64)[::2])
