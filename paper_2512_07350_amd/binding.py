@@ -71,12 +71,12 @@ class lp_adapter(C.Structure):
 
 class lp_norm(C.Structure):
     _fields_ = [("kind", C.c_int32), ("eps", C.c_float), ("weight", C.c_void_p), ("bias", C.c_void_p)]
-    holds, given = 1 << 31, ()          # rows that its tensors suffice for, see make_norm
+    holds, given = 1 << 31, {}          # rows that its tensors suffice for, see make_norm
 
 
 class lp_modulation(C.Structure):
     _fields_ = [("gate", C.c_void_p), ("scale", C.c_void_p), ("shift", C.c_void_p), ("stride", C.c_int64)]
-    holds, vectors, given = 1 << 31, 1 << 31, ()   # see make_modulation
+    holds, vectors, given = 1 << 31, 1 << 31, {}   # see make_modulation
 
 
 class LPError(RuntimeError):

@@ -231,3 +231,7 @@ def test_vectors_that_do_not_hold_the_requests_are_refused():
     _refused(m, gate=1 << 20)
     _refused(lp.make_norm, lp.LP_NORM_RMS, 1e-6, z(32, dtype=torch.float64))
     _refused(lp.make_norm, lp.LP_NORM_RMS, 1e-6, z(64)[::2])
+
+
+def test_a_width_past_32_bits_is_the_librarys_to_refuse():
+    _taken(lp.lp_norm_modulate, None, lp.LP_BF16, 1 << 20, lp.make_requests([0, 2]), 1 << 32, lp.make_norm(lp.LP_NORM_RMS, 1e-6), lp.make_modulation())
