@@ -407,7 +407,7 @@ int lp_norm_modulate(const void *x, int32_t x_type, void *y, const lp_requests *
  *   y[i]     = norm(h_out[i]) * (1 + scale[r]) + shift[r]
  * h, h_out: device, h_type, rows at i * stride_h and i * stride_h_out: the residual stream; h_out may be h (equal
  * strides).  u: device, bf16, rows at i * stride_u: what the half computed.  y: device, bf16, rows at i * stride_y;
- * NULL together with norm for the last residual, which nothing follows.  post: host, normalisation of u, or NULL for
+ * NULL together with norm for the last residual, which nothing follows (scale and shift are then not looked at).  post: host, normalisation of u, or NULL for
  * u itself.  y is formed from the binary32 sum, before it is rounded to h_type.  No other buffers may be the same.
  * Everything else as lp_norm_modulate.
  */

@@ -308,8 +308,8 @@ int check_norm(const lp_norm *n, int32_t *kind, float *eps, const float **weight
     return LP_OK;
 }
 
-// Types, width, requests and the vectors; *vec: whether these allow 16-byte pieces.
-int check_common(int32_t type, const lp_requests *requests, int32_t d, const lp_modulation *m, NormArgs *a) {
+// Types, width, requests and the vectors that the call uses: the others are not looked at, nor the stride where it uses none.
+int check_common(int32_t type, const lp_requests *requests, int32_t d, const lp_modulation *m, bool residual, bool norm, NormArgs *a) {
     if (type != LP_BF16 && type != LP_F32) return LP_ERR_INVALID_ARG;
     if (d < 1) return LP_ERR_INVALID_ARG;
     if (d > kMaxWidth) return LP_ERR_UNSUPPORTED;
@@ -318,13 +318,17 @@ int check_common(int32_t type, const lp_requests *requests, int32_t d, const lp_
     a->d = d;
     a->inv_d = 1.0f / float(d);
     a->n = int32_t(a->requests.rows());
-    if (m != nullptr && (m->gate != nullptr || m->scale != nullptr || m->shift != nullptr)) {
-        if (m->stride != 0 && m->stride < d) return LP_ERR_INVALID_ARG;
-        if (!aligned(m->gate, 4) || !aligned(m->scale, 4) || !aligned(m->shift, 4)) return LP_ERR_INVALID_ARG;
-        a->gate = m->gate;
-        a->scale = m->scale;
-        a->shift = m->shift;
-        a->stride_mod = m->stride;
+    if (m != nullptr) {
+        if (residual) a->gate = m->gate;
+        if (norm) {
+            a->scale = m->scale;
+            a->shift = m->shift;
+        }
+        if (a->gate != nullptr || a->scale != nullptr || a->shift != nullptr) {
+            if (m->stride != 0 && m->stride < d) return LP_ERR_INVALID_ARG;
+            if (!aligned(a->gate, 4) || !aligned(a->scale, 4) || !aligned(a->shift, 4)) return LP_ERR_INVALID_ARG;
+            a->stride_mod = m->stride;
+        }
     }
     return LP_OK;
 }
@@ -339,7 +343,7 @@ bool vectors_aligned(const NormArgs &a) {
 extern "C" int lp_norm_modulate(const void *x, int32_t x_type, void *y, const lp_requests *requests, int32_t d, int64_t stride_x,
                                 int64_t stride_y, const lp_norm *norm, const lp_modulation *modulation, void *stream) {
     NormArgs a{};
-    int rc = check_common(x_type, requests, d, modulation, &a);
+    int rc = check_common(x_type, requests, d, modulation, false, true, &a);
     if (rc != LP_OK) return rc;
     if (norm == nullptr || stride_x < d || stride_y < d) return LP_ERR_INVALID_ARG;
     if ((rc = check_norm(norm, &a.norm, &a.eps, &a.weight, &a.bias)) != LP_OK) return rc;
@@ -351,7 +355,6 @@ extern "C" int lp_norm_modulate(const void *x, int32_t x_type, void *y, const lp
     a.stride_x = stride_x;
     a.stride_y = stride_y;
     a.post = kNone;
-    a.gate = nullptr;
     const bool vec = vectors_aligned(a) && aligned16(x) && aligned16(y) && stride_x % 8 == 0 && stride_y % 8 == 0;
     return run(a, vec, x_type == LP_F32, false, static_cast<hipStream_t>(stream));
 }
@@ -360,14 +363,13 @@ extern "C" int lp_gated_residual_norm(const void *h, int32_t h_type, const void 
                                       int32_t d, int64_t stride_h, int64_t stride_u, int64_t stride_h_out, int64_t stride_y,
                                       const lp_norm *post, const lp_norm *norm, const lp_modulation *modulation, void *stream) {
     NormArgs a{};
-    int rc = check_common(h_type, requests, d, modulation, &a);
+    int rc = check_common(h_type, requests, d, modulation, true, norm != nullptr, &a);
     if (rc != LP_OK) return rc;
     if (stride_h < d || stride_u < d || stride_h_out < d || (norm != nullptr && stride_y < d)) return LP_ERR_INVALID_ARG;
     a.post = a.norm = kNone;
     if (post != nullptr && (rc = check_norm(post, &a.post, &a.post_eps, &a.post_weight, &a.post_bias)) != LP_OK) return rc;
     if (norm != nullptr && (rc = check_norm(norm, &a.norm, &a.eps, &a.weight, &a.bias)) != LP_OK) return rc;
     if ((norm == nullptr) != (y == nullptr) && a.n > 0) return LP_ERR_INVALID_ARG;
-    if (norm == nullptr) a.scale = a.shift = nullptr;
     if (a.n == 0) return LP_OK;
     const int size = h_type == LP_F32 ? 4 : 2;
     if (h == nullptr || u == nullptr || h_out == nullptr || !aligned(h, size) || !aligned(h_out, size) || !aligned(u, 2) || !aligned(y, 2))

@@ -235,3 +235,17 @@ def test_vectors_that_do_not_hold_the_requests_are_refused():
 
 def test_a_width_past_32_bits_is_the_librarys_to_refuse():
     _taken(lp.lp_norm_modulate, None, lp.LP_BF16, 1 << 20, lp.make_requests([0, 2]), 1 << 32, lp.make_norm(lp.LP_NORM_RMS, 1e-6), lp.make_modulation())
+
+
+def test_vectors_that_a_call_does_not_use_are_not_looked_at():
+    none = dict(req=lp.make_requests([0, 0]), x=None, y=None)                       # accepted: no rows, nothing is launched
+    m = lp.make_modulation
+    for vectors in (m(gate=64, stride=1), m(gate=66, stride=64), m(gate=66, scale=64, stride=64)):
+        assert _norm(mod=vectors, **none) == lp.LP_OK
+    last = dict(h=None, u=None, o=None, y=None, norm=None, starts=(0, 0))
+    for vectors in (m(scale=64, stride=1), m(scale=66, shift=65, stride=64), m(gate=64, scale=66, stride=64)):
+        assert _residual(mod=vectors, **last) == lp.LP_OK
+    # those that it uses are
+    assert _norm(mod=m(shift=66, stride=64), **none) == lp.LP_ERR_INVALID_ARG and _norm(mod=m(scale=64, stride=1), **none) == lp.LP_ERR_INVALID_ARG
+    assert _residual(mod=m(gate=66, stride=64), **last) == lp.LP_ERR_INVALID_ARG and _residual(mod=m(gate=64, stride=1), **last) == lp.LP_ERR_INVALID_ARG
+    assert _residual(mod=m(scale=66, stride=64), **dict(last, norm="rms")) == lp.LP_ERR_INVALID_ARG
