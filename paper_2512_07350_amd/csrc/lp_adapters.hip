@@ -359,7 +359,7 @@ extern "C" int lp_qkv_projection_adapters(const void *x, const void *w_qkv, cons
         !aligned16(k) || !aligned16(v))
         return LP_ERR_INVALID_ARG;
     if (q == k || q == v || k == v || q == x || k == x || v == x) return LP_ERR_INVALID_ARG;
-    if (workspace != nullptr && (workspace == x || workspace == w_qkv || workspace == q || workspace == k || workspace == v)) return LP_ERR_INVALID_ARG;
+    if (runs.largest > 0 && (workspace == x || workspace == w_qkv || workspace == q || workspace == k || workspace == v)) return LP_ERR_INVALID_ARG;
     AdaptedArgs<true> a{};
     a.requests = runs.requests.count;
     int first = -1;

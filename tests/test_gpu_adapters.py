@@ -478,3 +478,21 @@ def test_the_blocks_of_two_requests_from_a_graph():
     hw = h.double() + spread(mod[:, 2]) * y.double()
     close(h_out, hw, 2.0 ** -12 * float(hw.abs().max()))
     close(last, layer(hw) * (1 + spread(mod[:, 3])) + spread(mod[:, 4]), 2.0 ** -12)
+
+
+def test_a_workspace_is_not_looked_at_without_adapters():
+    """Neither where it lies nor how large it is."""
+    import torch
+    c = Qkv([(3, 5, 7), (2, 9, 4)], [0, 0], 4, 64)
+    want = c.run()
+    out = [torch.empty_like(t) for t in want]
+    ropes = [lp.make_rope(g, o, c.split, c.base, c.hd) for g, o in zip(c.grids, c.offsets)]
+    st = torch.cuda.current_stream().cuda_stream
+    for ws in (c.x, c.w, out[0], out[2], c.x.data_ptr() + 2):
+        lp.lp_qkv_projection_adapters(c.x, c.w, c.bias, c.gains[0], c.gains[1], EPS, ropes, *out, lp.make_requests(c.starts), c.heads, c.hd,
+                                      lp.make_adapters(c.adapters), ws, 3, st)
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+        lin = Case(c.lengths, [0, 0], 256, 256)
+        y = torch.empty(lin.n, 256, dtype=torch.bfloat16, device="cuda")
+        lp.lp_linear_adapters(lin.x, lin.w, lin.bias, y, lp.make_requests(lin.starts), 256, 256, lp.make_adapters(lin.adapters), y, 3, st)
+        assert torch.equal(y, lin.linear())
