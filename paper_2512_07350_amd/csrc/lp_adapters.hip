@@ -12,6 +12,7 @@
 // launch (product_few); with more ranks two, 6 rows of d_in 1536 and rank 128 13.3 us, 5.4 without adapters.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "lp_gemm.h"
@@ -271,7 +272,7 @@ int project(AdaptedArgs<QKV> &a, Runs &runs, void *workspace, int64_t workspace_
         d.t_blocks = (runs.largest + kRanks - 1) / kRanks;
         const int rc = run_down(d, runs.runs, dev, cus, stream);
         if (rc != LP_OK) return rc;
-    a.control = d.control;
+        a.control = d.control;
         a.t = d.t;
         a.t_row = d.t_row;
         a.t_blocks = d.t_blocks;
@@ -281,19 +282,14 @@ int project(AdaptedArgs<QKV> &a, Runs &runs, void *workspace, int64_t workspace_
 
 }  // namespace
 
-// For the tests, as lp_internal_gemm_way: rows and ranks of the requests; way[6], way[7]: rows of D and tokens of the down products' tile (0, 0: one launch).
-extern "C" int lp_internal_adapted_way(const int64_t *start, const int32_t *rank, int32_t count, int32_t d_in, int32_t d_out, int32_t head_dim,
-                                       int32_t cus, int64_t way[8]) {
-    DownArgs d{};
-    d.sections = head_dim == 0 ? 1 : 3;
-    int runs = 0;
-    for (int r = 0; r < count; ++r)
-        if (start[r + 1] > start[r]) d.run[runs++] = DownRun{int32_t(start[r]), rank[r], 0, 0, 0.0f, nullptr, nullptr};
-    d.run[runs] = DownRun{int32_t(start[count]), 0, 0, 0, 0.0f, nullptr, nullptr};
-    const int64_t n = start[count];
-    const Plan p = pick_adapted(int32_t(n), d_in, d_out, head_dim, cus, runs, d.run);
-    plan_way(p, n, d_out, head_dim == 0 && four_waves(p, d_in), way);
-    if (takes_few(n, d_out, head_dim, cus, runs, d.run)) {
+extern "C" int lp_internal_adapted_call_way(const lp_requests *requests, const lp_adapter *adapters, int32_t d_in, int32_t d_out, int32_t head_dim,
+                                            int32_t cus, int64_t way[8]) {
+    Runs runs;
+    const int rc = make_runs(requests, adapters, d_in, d_out, head_dim == 0 ? 1 : 3, &runs);
+    if (rc != LP_OK) return rc;
+    const int64_t n = runs.requests.rows();
+    DownArgs &d = runs.down;
+    if (takes_few(n, d_out, head_dim, cus, runs.runs, d.run)) {
         way[0] = Split64x32::kF;
         way[1] = Split64x32::kT;
         way[2] = way[3] = way[6] = way[7] = 0;
@@ -301,10 +297,21 @@ extern "C" int lp_internal_adapted_way(const int64_t *start, const int32_t *rank
         way[5] = Split64x32::kThreads;
         return LP_OK;
     }
-    const Down down = pick_down(d, runs, cus);
+    const Plan p = pick_adapted(int32_t(n), d_in, d_out, head_dim, cus, runs.runs, d.run);
+    plan_way(p, n, d_out, head_dim == 0 && four_waves(p, d_in), way);
+    const Down down = pick_down(d, runs.runs, cus);
     way[6] = down == kDownFew ? DownFew::kF : down == kDownMany ? DownMany::kF : DownTall::kF;
     way[7] = down == kDownFew ? DownFew::kT : down == kDownMany ? DownMany::kT : DownTall::kT;
     return LP_OK;
+}
+
+extern "C" int lp_internal_adapted_way(const int64_t *start, const int32_t *rank, int32_t count, int32_t d_in, int32_t d_out, int32_t head_dim,
+                                       int32_t cus, int64_t way[8]) {
+    lp_adapter adapters[LP_MAX_REQUESTS];
+    for (int r = 0; r < std::min(count, LP_MAX_REQUESTS); ++r)           // addresses that nothing reads, no two alike
+        adapters[r] = lp_adapter{reinterpret_cast<const void *>(uintptr_t(32 * r + 16)), reinterpret_cast<const void *>(uintptr_t(32 * r + 32)), rank[r], 1.0f};
+    const lp_requests requests{count, start};
+    return lp_internal_adapted_call_way(&requests, adapters, d_in, d_out, head_dim, cus, way);
 }
 
 extern "C" int64_t lp_adapter_workspace_size(int64_t n_tokens, int32_t rank, int32_t sections) {

@@ -40,6 +40,12 @@ int lp_internal_attention_rows_split(uint64_t k, uint64_t v, int64_t stride_tok,
 // head_dim 0: lp_linear.  way: features and tokens of a tile, those of the tiles that cut the last round (0: none),
 // the workgroups, and the threads of each.
 int lp_internal_gemm_way(int64_t n, int32_t d_in, int32_t d_out, int32_t head_dim, int32_t cus, int64_t way[6]);
+// The same for the calls with adapters (head_dim 0: lp_linear_adapters), which take neighbours with one adapter as one run; way[6], way[7]: rows of
+// D and tokens of the down products' tile (0, 0: one launch).  The second: requests with an adapter of their own each, of these ranks.
+int lp_internal_adapted_call_way(const lp_requests *requests, const lp_adapter *adapters, int32_t d_in, int32_t d_out, int32_t head_dim,
+                                 int32_t cus, int64_t way[8]);
+int lp_internal_adapted_way(const int64_t *start, const int32_t *rank, int32_t count, int32_t d_in, int32_t d_out, int32_t head_dim,
+                            int32_t cus, int64_t way[8]);
 }
 
 #ifdef __HIPCC__

@@ -46,3 +46,14 @@ def gemm(n, d_in, d_out, head_dim=0, cus=None):
     way = (C.c_int64 * 6)()
     assert fn(n, d_in, d_out, head_dim, _cus(cus), way) == 0
     return GemmWay((way[0], way[1]), (way[2], way[3]) if way[2] else None, way[4], way[5])
+
+
+def adapted(requests, adapters, d_in, d_out, head_dim=0, cus=None):
+    """What a call with adapters (make_requests, make_adapters or addresses) runs, and rows of D and tokens of the down products' tile ((0, 0): one
+    launch for all).  head_dim 0: lp_linear_adapters, else lp_qkv_projection_adapters (d_out = 3 d_in)."""
+    fn = lp._lib().lp_internal_adapted_call_way
+    fn.argtypes = [C.POINTER(lp.lp_requests), C.POINTER(lp.lp_adapter)] + [C.c_int32] * 4 + [C.POINTER(C.c_int64)]
+    fn.restype = C.c_int
+    way = (C.c_int64 * 8)()
+    assert fn(requests, adapters, d_in, d_out, head_dim, _cus(cus), way) == 0
+    return GemmWay((way[0], way[1]), (way[2], way[3]) if way[2] else None, way[4], way[5]), (way[6], way[7])

@@ -496,3 +496,20 @@ def test_a_workspace_is_not_looked_at_without_adapters():
         y = torch.empty(lin.n, 256, dtype=torch.bfloat16, device="cuda")
         lp.lp_linear_adapters(lin.x, lin.w, lin.bias, y, lp.make_requests(lin.starts), 256, 256, lp.make_adapters(lin.adapters), y, 3, st)
         assert torch.equal(y, lin.linear())
+
+
+@pytest.mark.parametrize("same,one_launch", [(True, True), (False, False)])
+def test_the_internal_say_on_a_call_is_what_it_runs(same, one_launch):
+    """A call of one launch leaves its workspace as it was; the first launch of two writes its beginning.  Two requests of 64 ranks in one tile: one
+    launch if they have one adapter."""
+    import torch
+    c = Case([10, 10], [64, 64], 512, 512, seed=41)
+    if same:
+        c.adapters[1] = c.adapters[0]
+    req, table = lp.make_requests(c.starts), lp.make_adapters(c.adapters)
+    assert (routes.adapted(req, table, 512, 512)[1] == (0, 0)) == one_launch
+    y, (ws, size) = torch.empty(c.n, 512, dtype=torch.bfloat16, device="cuda"), c.workspace()
+    lp.lp_linear_adapters(c.x, c.w, c.bias, y, req, 512, 512, table, ws, size, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert bool(torch.isnan(ws.float()).all()) == one_launch
+    inside(y, *c.want())
