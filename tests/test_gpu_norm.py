@@ -333,3 +333,21 @@ def test_infinite_vectors_where_no_bias_stands(d, norm, post):
     others = [0, 1, 5, 6]
     wy, oy = c.modulate(want, off)
     _inside(y.float().cpu().numpy()[others], wy[others], oy[others], HALF["bf16"], "y")
+
+
+# 1024 threads to a row whose last pieces lie partly or wholly past its end, in whole pieces and in single elements
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [8200, 8201, 9001, 12288, 12296, 16376])
+def test_widths_between_8192_and_16384(d, x):
+    Case([3, 0, 2], d, x, "layer").check_norm((8, 16), extra=1)
+    Case([1, 4], d, x, "rms", post="layer").check_residual((8, 0, 16, 8), extra=1)
+
+
+@pytest.mark.parametrize("d", [7001, 8192, 9001, 12296])
+def test_several_wide_rows_to_a_workgroup(d):
+    """512 and 1024 threads to a row: every workgroup takes two or three, which belong to one request or to several; four sums to a row."""
+    import torch
+    lengths = [600, 1, 0, 1, 1, 400, 300]
+    assert sum(lengths) > 4 * torch.cuda.get_device_properties(0).multi_processor_count
+    Case(lengths, d, "bf16", "layer").check_norm()
+    Case(lengths, d, "f32", "layer", "layer").check_residual()
