@@ -513,3 +513,109 @@ def test_the_internal_say_on_a_call_is_what_it_runs(same, one_launch):
     torch.cuda.synchronize()
     assert bool(torch.isnan(ws.float()).all()) == one_launch
     inside(y, *c.want())
+
+
+# ---- calls of two launches
+
+def test_merged_runs_of_two_launches():
+    """Neighbours with one adapter, a request without rows between them, are one run in the down products and the k-tiles too."""
+    import torch
+    c = Case([2000, 0, 3110, 77], [72, 16, 72, 0], 576, 896, seed=51)
+    c.adapters[2] = c.adapters[0]
+    ways = routes.adapted(lp.make_requests(c.starts), lp.make_adapters(c.adapters), c.d_in, c.d_out)
+    assert ways[1] != (0, 0)
+    y = c.linear()
+    rows = torch.tensor(sorted(set(range(0, c.n, 17)) | {1999, 2000, 2001, 5109, 5110, 5186}), device="cuda")
+    inside(y[rows], *c.want(rows))
+    joined = Case([5110, 77], [72, 0], 576, 896)
+    joined.x, joined.w, joined.bias, joined.adapters = c.x, c.w, c.bias, [c.adapters[0], None]
+    assert routes.adapted(lp.make_requests(joined.starts), lp.make_adapters(joined.adapters), c.d_in, c.d_out) == ways
+    assert torch.equal(y, joined.linear())
+
+
+def test_one_workspace_for_the_calls_of_a_stream():
+    """q | k | v, then a projection with other adapters of other requests, in one workspace, again and again with nothing between them: eager, and
+    from a graph that replays with eager calls in the same workspace between."""
+    import torch
+    q = Qkv([(3, 20, 20), (5, 9, 11), (1, 1, 1)], [72, 0, 40], 4, 64, seed=52)
+    o = Case([900, 0, 595, 200, 1], [16, 8, 128, 32, 0], 256, 256, seed=53)
+    p = Case([q.n], [96], 256, 256, seed=54)
+    tables = [lp.make_adapters(c.adapters) for c in (q, o, p)]
+    requests = [lp.make_requests(c.starts) for c in (q, o, p)]
+    for c, r, t, hd in zip((q, o, p), requests, tables, (64, 0, 0)):
+        assert routes.adapted(r, t, c.d_in, c.d_out, hd)[1] != (0, 0)
+    want = [*q.run(), o.linear(), p.linear()]             # a workspace each
+    size = max(lp.lp_adapter_workspace_size(q.n, 72, 3), lp.lp_adapter_workspace_size(o.n, 128, 1), lp.lp_adapter_workspace_size(p.n, 96, 1))
+    ws = torch.full((size // 2 + 64,), float("nan"), dtype=torch.bfloat16, device="cuda")
+    out = [torch.empty_like(t) for t in want]
+    ropes = [lp.make_rope(g, off, q.split, q.base, q.hd) for g, off in zip(q.grids, q.offsets)]
+
+    def calls():
+        st = torch.cuda.current_stream().cuda_stream
+        lp.lp_qkv_projection_adapters(q.x, q.w, q.bias, q.gains[0], q.gains[1], EPS, ropes, *out[:3], requests[0], q.heads, q.hd, tables[0], ws, size, st)
+        lp.lp_linear_adapters(o.x, o.w, o.bias, out[3], requests[1], o.d_in, o.d_out, tables[1], ws, size, st)
+        lp.lp_linear_adapters(p.x, p.w, p.bias, out[4], requests[2], p.d_in, p.d_out, tables[2], ws, size, st)
+
+    def check():
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want)) and torch.isnan(ws[size // 2:].float()).all()
+        for t in out:
+            t.fill_(77.0)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(3):
+            calls()
+    side.synchronize()
+    check()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        calls()
+        calls()
+    for _ in range(4):
+        graph.replay()
+        check()
+        calls()
+        check()
+
+
+@pytest.mark.parametrize("value", ["inf", "nan"])
+@pytest.mark.parametrize("n,d_in,d_out,tiles", [
+    (1438, 1024, 1152, "128x64"), (1345, 576, 1536, "128x128"), (12001, 1024, 384, "256x128"), (3783, 128, 3840, "256x256"), (3600, 128, 4608, "256x256+128x64"),
+    (4033, 2112, 1536, "256x128"), (2560, 4096, 6144, "256x256"), (4097, 2112, 4224, "256x256+128x128"), (6145, 2176, 3584, "256x256+256x128"),
+])
+def test_an_adapter_that_is_not_finite_on_large_tiles(n, d_in, d_out, tiles, value):
+    """U of the second of four requests, whose edges lie inside tiles: its rows are NaN throughout, the others as ever."""
+    import torch
+    lengths = [n // 3 + 5, n // 4, n // 5, 0]
+    lengths[3] = n - sum(lengths)
+    c = Case(lengths, [72, 40, 16, 32], d_in, d_out, seed=55)
+    ways = way(c.lengths, c.ranks, d_in, d_out)
+    assert str(ways[0]) == tiles and ways[1] != (0, 0) and ways[0].threads == (256 if d_in >= 2112 else 512)
+    c.adapters[1][1].view(-1)[-1 if value == "inf" else d_out * 20 + 3] = float(value)
+    y = c.linear()
+    a, b = c.starts[1], c.starts[2]
+    assert torch.isnan(y[a:b].float()).all()
+    edges = [s + i for s in c.starts for i in (-2, -1, 0, 1)]
+    rows = torch.tensor([r for r in sorted(set(edges) | set(range(0, n, max(1, n // 300)))) if 0 <= r < n and not a <= r < b], device="cuda")
+    inside(y[rows], *c.want(rows))
+    assert torch.isfinite(y[:a].float()).all() and torch.isfinite(y[b:].float()).all()
+
+
+@pytest.mark.parametrize("heads,hd,grid,tiles", [(8, 128, (3, 20, 20), "128x128"), (4, 128, (9, 23, 13), "256x128"), (8, 64, (11, 33, 15), "256x256"),
+                                                 (12, 128, (9, 20, 20), "256x256+128x64")])
+def test_a_qkv_adapter_that_is_not_finite_on_large_tiles(heads, hd, grid, tiles):
+    import torch
+    t = grid[0]
+    c = Qkv([(a,) + grid[1:] for a in (t - t // 2 - t // 3, t // 3, t // 2)], [72, 24, 40], heads, hd, seed=56)
+    ways = way(c.lengths, c.ranks, c.d_in, c.d_out, hd)
+    assert str(ways[0]) == tiles and ways[1] != (0, 0)
+    c.adapters[1][1][2 * c.d_in + 5, 7] = float("inf")     # of v
+    want = [x.clone() for x in c.run()]
+    a, b = c.starts[1], c.starts[2]
+    assert torch.isnan(want[2][a:b].float()).all()
+    clean = Qkv(c.grids, [72, 24, 40], heads, hd, seed=56)
+    clean.check()
+    for got, fine in zip(want, clean.run()):
+        assert torch.equal(got[:a], fine[:a]) and torch.equal(got[b:], fine[b:])
