@@ -340,7 +340,8 @@ typedef struct lp_adapter {
  * of other requests are not affected.
  * One small launch for the down products, whose results are kept as two bf16 each (2^-17 relative), then one for
  * the rest: the adapters are further terms of w's sums, in binary32, with one rounding to bf16 on store.  With few
- * rows and ranks one launch does both.  A call's results are the same every time; in another batch a row may differ in its last
+ * rows and ranks one launch does both.  A stretch of rows costs by the adapters in it, 32 ranks of each at a time: dozens of requests of a row
+ * or two, packed beside each other with an adapter each, lengthen a large call.  A call's results are the same every time; in another batch a row may differ in its last
  * bit, where the sums are formed in another order (lp_norm_modulate and lp_gated_residual_norm give a row the same
  * result in every batch of one alignment).
  */
@@ -408,7 +409,7 @@ int lp_norm_modulate(const void *x, int32_t x_type, void *y, const lp_requests *
  * h, h_out: device, h_type, rows at i * stride_h and i * stride_h_out: the residual stream; h_out may be h (equal
  * strides).  u: device, bf16, rows at i * stride_u: what the half computed.  y: device, bf16, rows at i * stride_y;
  * NULL together with norm for the last residual, which nothing follows (scale and shift are then not looked at).  post: host, normalisation of u, or NULL for
- * u itself.  y is formed from the binary32 sum, before it is rounded to h_type.  No other buffers may be the same.
+ * u itself.  y is formed from the binary32 sum, before it is rounded to h_type.  Neither h_out nor y may be another of the buffers.
  * Everything else as lp_norm_modulate.
  */
 int lp_gated_residual_norm(const void *h, int32_t h_type, const void *u, void *h_out, void *y, const lp_requests *requests,

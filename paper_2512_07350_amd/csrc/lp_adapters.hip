@@ -161,7 +161,10 @@ int make_runs(const lp_requests *requests, const lp_adapter *adapters, int32_t d
     return LP_OK;
 }
 
-// The tiling of a call: pick_plan's, with the k-tiles of the adapters that a tile of t tokens takes on average.
+// The tiling of a call: pick_plan's, with the k-tiles of the adapters that a tile of t tokens takes on average.  A tile that many short runs
+// crowd takes more, every one of them a k-tile for 32 ranks: 48 requests of one row beside 20000 rows, all of rank 128, 1536 -> 1536, take 333 us in
+// 256 x 256 tiles (199 to 283 by where the 48 lie in 128 x 128, the rest of them in 128 x 64), 62 of rank 256 710 (283 to 577).  With the longest tile in
+// the price these took 206 to 290 and 431 to 665, and 20 of 1500 ordinary calls, whose tiling it changed, 0.78 to 1.14 of their time, 1.03 on average.
 Plan pick_adapted(int32_t n, int32_t d_in, int32_t d_out, int32_t head_dim, int cus, int32_t runs, const DownRun *run) {
     return pick_plan(n, d_out, small_tilings(head_dim), cus, [&](int t) {
         int64_t extra = 0;
@@ -224,7 +227,8 @@ int run_down(DownArgs &d, int32_t runs, int dev, int cus, hipStream_t stream) {
     }
 }
 
-// Whether a call is taken in one launch (product_few): one round of 64 x 32 tiles at most, and in each of them ranks for one product of 64 rows.
+// Whether a call is taken in one launch (product_few): one round of 64 x 32 tiles at most, in each of them ranks for one product of 64 rows, as many
+// runs as the arguments hold; heads of 64 features (a tile's).
 // us of one launch / of two: 320 x 1536 -> 1536 10.0 / 13.9, 4000 x 4096 -> 128 17.6 / 25.8, 96 x 6144 -> 5120 26.5 / 30.3, 2000 x 256 -> 256 6.4 / 9.5; in
 // two rounds 400 x 1536 -> 1536 18.9 / 14.1, 1000 x 512 -> 1536 11.9 / 11.3, 6000 x 4096 -> 128 33.3 / 28.6.
 bool takes_few(int64_t n, int32_t d_out, int32_t head_dim, int cus, int32_t runs, const DownRun *run) {

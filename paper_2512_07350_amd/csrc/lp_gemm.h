@@ -802,11 +802,12 @@ __device__ __forceinline__ void product_split_k(uint32_t lds0, const Args &a, in
 }
 
 // Calls of few rows in one launch.  Every workgroup of 64 features x 32 tokens forms t of its tokens itself, for the ranks of the runs that have rows
-// in its tile one after the other (at most 64): its product has 64 rows more, those of the D's, a group of 8 to a load; then
+// in its tile one after the other (at most 64, of at most 32 runs in the call): its product has 64 rows more, those of the D's, a group of 8 to a load; then
 //   y += sum_j U[feature, j] (hi + lo)[token, j],
 // t being zero where the token is not of j's run.  It costs D in every workgroup, and saves the launch in front and the trip through memory:
-// 6 rows of d_in 1536 in two launches 12.5 us, with the two products one after the other 10.1, as one 9.6 (eight stages 9.9; without adapters 5.4); q | k | v
-// of 306 x 256 10.5, 8.5, 7.9.
+// 6 rows of d_in 1536 in two launches 12.8 us, with the two products one after the other 10.5, as one 10.1 (eight stages 3 % more; without adapters
+// 5.4); q | k | v of 306 x 256 10.5, 8.5, 7.9.  Not for heads of 128 features, which do not fit the tile: one row of 12 heads of 128 takes 17.4 us in two
+// launches, of 24 heads of 64 10.9 in one.
 //
 // LDS behind the stages: t as kFewRanks / 32 times hi and lo, 32 tokens of 32 ranks; U as 64 features of 32 ranks; the runs whose U is not finite.
 using FewTile = Tiling<2, 2, 4, 1, 6, kSplitK>;          // of W's 64 features and the D's 64 rows
@@ -934,7 +935,8 @@ __device__ __forceinline__ void product_few(uint32_t lds0, const Args &a, int f0
     }
 }
 
-// Coordinates of token tk in its request's grid; the lanes' tokens lie between `first` and `last`, mostly of one request.
+// Coordinates of token tk in its request's grid; the lanes' tokens lie between `first` and `last`, mostly of one request.  The grids are fetched here, in the
+// epilogue, and divided by as they are: 19052 x 1536 of one request without adapters takes 238 us, 233 where the grid is the call's; 13230 x 5120 1538 and 1530.
 __device__ __forceinline__ void grid_position(const AdaptedArgs<true> &a, int32_t tk, int32_t first, int32_t last, float &t, float &h, float &w) {
     const int lane = threadIdx.x % 64;
     const int32_t start = lane < a.requests ? a.grid[lane].start : INT32_MAX;
@@ -1330,7 +1332,8 @@ bool four_waves(const Plan &p, int32_t d_in) { return p.tile <= 1 && d_in / kBK 
 template <bool QKV, int HD, typename Args>
 int launch_plan(const Plan &p, const Args &a, hipStream_t stream) {
     constexpr bool kSmall = small_tilings(QKV ? HD : 0);
-    // two workgroups of 64 x 64 fill a compute unit's LDS: with the adapters' tables a stage less does
+    // two workgroups of 64 x 64 fill a compute unit's LDS: with the adapters' tables a stage less does.  The price is that of five: of 40 calls with
+    // adapters in 64 x 64 tiles the other tilings are faster by 1 % in one; five stages, one workgroup to a unit, 0.94 to 1.04 of the time, 1.00 on average
     using Tile64 = std::conditional_t<kAdapted<Args>, Tiling<2, 2, 2, 2, 4>, Tile64x64>;
     if constexpr (!QKV) {
         if (four_waves(p, a.d_in)) {
