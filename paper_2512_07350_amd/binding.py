@@ -357,14 +357,16 @@ def make_requests(starts) -> lp_requests:
     return r
 
 
+_BF16 = {"bfloat16", "int16", "uint16"}     # bf16 may come as its 16-bit words
+_F32 = {"float32"}
+
+
 def _typed(t, types, what: str) -> None:
-    """bf16 may come as its 16-bit words."""
-    if str(t.dtype) not in types:
-        raise ValueError("%s: %s, not %s" % (what, types[0], t.dtype))
-
-
-_BF16 = ("torch.bfloat16", "torch.int16", "torch.uint16")
-_F32 = ("torch.float32",)
+    """A tensor's type is of these: their names, and once met themselves."""
+    if t.dtype not in types:
+        if str(t.dtype) not in {"torch.%s" % name for name in types if isinstance(name, str)}:
+            raise ValueError("%s: %s for %s" % (what, t.dtype, "bfloat16" if types is _BF16 else "float32"))
+        types.add(t.dtype)
 
 
 def make_adapters(adapters):
@@ -377,14 +379,14 @@ def make_adapters(adapters):
             down, up, scale = ad
             if down.dim() != 2 or up.dim() != 2 or not (down.is_contiguous() and up.is_contiguous()):
                 raise ValueError("adapter %d: down [sections * rank, d_in] and up [d_out, rank], contiguous" % i)
-            rows, rank = int(down.shape[0]), int(up.shape[1])
+            (rows, d_in), (d_out, rank), at = down.shape, up.shape, down.data_ptr()
             if rows % rank if rank else rows:
                 raise ValueError("adapter %d: down [sections * rank, d_in] and up [d_out, rank], contiguous" % i)
             _typed(down, _BF16, "adapter %d" % i)
             _typed(up, _BF16, "adapter %d" % i)
-            out[i] = lp_adapter(_ptr(down), _ptr(up), rank, float(scale))
+            out[i] = lp_adapter(at, up.data_ptr(), rank, float(scale))
             if rank:
-                out.given[i] = (out[i].down, (rows // rank, int(down.shape[1]), int(up.shape[0])))
+                out.given[i] = (at or None, (rows // rank, d_in, d_out))
     sizes = {g[1] for g in out.given if g}
     out.sizes = sizes.pop() if len(sizes) == 1 else None     # of all alike
     return out
@@ -444,7 +446,7 @@ def make_norm(kind: int, eps: float, weight=None, bias=None) -> lp_norm:
             _typed(t, _F32, name)
             if not t.is_contiguous():
                 raise ValueError("%s has to be contiguous" % name)
-            given[name] = (getattr(norm, name), int(t.numel()))
+            given[name] = (t.data_ptr() or None, t.numel())
     if given:
         norm.holds, norm.given = min(n for _, n in given.values()), given
     return norm
@@ -459,26 +461,30 @@ def _check_norm(norm: lp_norm, d: int) -> None:
 def make_modulation(gate=None, scale=None, shift=None, stride: Optional[int] = None) -> lp_modulation:
     """Vectors per request, device, binary32, which the caller keeps.  stride defaults to the row stride that the tensors
     given have in common; a vector (one dimension) is that of every request."""
-    tensors = {k: t for k, t in (("gate", gate), ("scale", scale), ("shift", shift)) if t is not None and not isinstance(t, int)}
-    for name, t in tensors.items():
-        if t.stride(-1) != 1:
+    tensors = [(k, t, t.stride(), t.shape) for k, t in (("gate", gate), ("scale", scale), ("shift", shift)) if t is not None and not isinstance(t, int)]
+    for name, t, strides, _ in tensors:
+        if strides[-1] != 1:
             raise ValueError("a request's vector has to be contiguous")
         _typed(t, _F32, name)
     if stride is None:
-        if any(isinstance(t, int) for t in (gate, scale, shift)):
+        if isinstance(gate, int) or isinstance(scale, int) or isinstance(shift, int):
             raise ValueError("addresses need a stride")
-        strides = {int(t.stride(0)) if t.dim() > 1 else 0 for t in tensors.values()}
-        if len(strides) > 1:
-            raise ValueError("gate, scale and shift need one row stride: %s" % sorted(strides))
-        stride = strides.pop() if strides else 0
-    m = lp_modulation(_ptr(gate) or None, _ptr(scale) or None, _ptr(shift) or None, int(stride))
+        of_rows = {strides[0] if len(strides) > 1 else 0 for _, _, strides, _ in tensors}
+        if len(of_rows) > 1:
+            raise ValueError("gate, scale and shift need one row stride: %s" % sorted(of_rows))
+        stride = of_rows.pop() if of_rows else 0
+    stride = int(stride)
+    m = lp_modulation(_ptr(gate) or None, _ptr(scale) or None, _ptr(shift) or None, stride)
     given = {}                              # tensor's address, vectors, elements of one, and elements in memory by field
-    for name, t in tensors.items():
-        own = t.dim() > 1
-        vectors, elements = (int(t.shape[0]), int(t[:1].numel())) if own and m.stride else (1 << 31, int(t[:1].numel() if own else t.numel()))
-        if m.stride != (int(t.stride(0)) if own else 0):     # the caller's own stride over the tensor's memory: known with d
-            vectors = 0
-        given[name] = (getattr(m, name), vectors, elements, t.untyped_storage().nbytes() // 4 - t.storage_offset())
+    for name, t, strides, shape in tensors:
+        many, vectors, elements, room = len(shape) > 1, 1 << 31, t.numel(), 0
+        if many:
+            elements //= shape[0] or 1
+            if stride:
+                vectors = shape[0]
+        if stride != (strides[0] if many else 0):            # the caller's own stride over the tensor's memory: known with d
+            vectors, room = 0, t.untyped_storage().nbytes() // 4 - t.storage_offset()
+        given[name] = (t.data_ptr() or None, vectors, elements, room)
     if given:
         m.vectors, m.holds, m.given = min(g[1] for g in given.values()), min(g[2] for g in given.values()), given
     return m
