@@ -442,7 +442,7 @@ def make_norm(kind: int, eps: float, weight=None, bias=None) -> lp_norm:
     norm = lp_norm(int(kind), float(eps), _ptr(weight) or None, _ptr(bias) or None)
     given = {}                              # tensor's address and elements by field
     for name, t in (("weight", weight), ("bias", bias)):
-        if t is not None and not isinstance(t, int):
+        if hasattr(t, "dtype"):
             _typed(t, _F32, name)
             if not t.is_contiguous():
                 raise ValueError("%s has to be contiguous" % name)

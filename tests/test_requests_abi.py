@@ -249,3 +249,12 @@ def test_vectors_that_a_call_does_not_use_are_not_looked_at():
     assert _norm(mod=m(shift=66, stride=64), **none) == lp.LP_ERR_INVALID_ARG and _norm(mod=m(scale=64, stride=1), **none) == lp.LP_ERR_INVALID_ARG
     assert _residual(mod=m(gate=66, stride=64), **last) == lp.LP_ERR_INVALID_ARG and _residual(mod=m(gate=64, stride=1), **last) == lp.LP_ERR_INVALID_ARG
     assert _residual(mod=m(scale=66, stride=64), **dict(last, norm="rms")) == lp.LP_ERR_INVALID_ARG
+
+
+def test_a_norm_takes_anything_that_has_an_address():
+    class Buffer:
+        def data_ptr(self):
+            return 1 << 20
+    norm = lp.make_norm(lp.LP_NORM_LAYER, 1e-6, Buffer(), 1 << 21)
+    assert (norm.weight, norm.bias) == (1 << 20, 1 << 21)
+    _taken(lp.lp_norm_modulate, None, lp.LP_BF16, 1 << 20, lp.make_requests([0, 2]), 64, norm)
